@@ -251,8 +251,16 @@ def _bits(x):
     return x.view(torch.int32)
 
 
+def _mixed(step):
+    """The step's part of the dither: 32 bits that change as if drawn from step to step."""
+    h = step * 0x9E3779B9 & 0xFFFFFFFF
+    h = (h ^ h >> 15) * 0x6A09E667 & 0xFFFFFFFF
+    h = (h ^ h >> 13) * 0x9E3779B9 & 0xFFFFFFFF
+    return h ^ h >> 16
+
+
 def _dither(N, step, turn, device):
-    u = torch.arange(N, device=device) * 0x6A09E667 + step * 0x9E3779B9 + turn
+    u = torch.arange(N, device=device) * 0x6A09E667 + _mixed(step) + turn
     return ((u & 0xFFFFFFFF) >> 12).to(torch.int32)
 
 
@@ -395,7 +403,10 @@ def _grid(x, top, above_zero, step, turn, first):
     field = (torch.frexp(y)[1] + 126).clamp(min=1)
     ulp = torch.pow(torch.tensor(2.0, dtype=torch.float64, device=x.device), (field - 130).double())
     i = torch.arange(first, first + full.numel(), device=x.device, dtype=torch.int64)
-    u = (i * 0x6A09E667 + step * 0x9E3779B9 + turn) % (1 << 32)
+    h = 2654435769 * step % 2 ** 32
+    h = 1779033703 * (h ^ h // 2 ** 15) % 2 ** 32
+    h = 2654435769 * (h ^ h // 2 ** 13) % 2 ** 32
+    u = (i * 1779033703 + (h ^ h // 2 ** 16) + turn) % 2 ** 32
     k = torch.floor(y / ulp + (u // 4096).double().view_as(y) / (1 << 20))
     k = torch.where((k < 1) & (y > 0) & above_zero, 1.0, k)
     return (k * ulp * shift).view(-1)
