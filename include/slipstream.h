@@ -439,6 +439,155 @@ int32_t ss_embbag_ln_backward(const ss_tables *tables, const int32_t *idx, int32
                               size_t ws_bytes, void *stream);
 
 /*
+ * The dense side of an iteration: what surrounds the tables in a model whose other parameters are
+ * trained with AdamW.  Element types of these calls:
+ */
+enum { SS_F32 = 0, SS_BF16 = 1, SS_F16 = 2 };
+
+/*
+ * Many tensors at once.  A list names the tensors of a model once; the calls below then take all
+ * of them in one launch each.  Tensors are contiguous and start at any address their type allows
+ * (views of one flat buffer, say); no two parameters of a list overlap.
+ *
+ * ss_tensor_list_plan (host arithmetic only) sets num_tensors, num_chunks and state_elems of *list
+ * (list->chunks is left alone) and, if `chunks` is not NULL, writes the num_chunks * SS_CHUNK_BYTES
+ * bytes of the list's work table there.  The caller copies them to device memory (8-byte aligned)
+ * and sets list->chunks to that copy; the table holds no address, only sizes and types.  A list
+ * of up to 2^31 - 1 chunks (of 2048 elements at least) is taken.
+ * Per-element arrays that go with a list (moments, master copies) hold the tensors one after the
+ * other, each padded to a multiple of SS_MOMENT_BLOCK elements: state_elems in all, tensor k's at
+ * sum_{j<k} round_up(numel_j, SS_MOMENT_BLOCK).  Padding stays as it was or becomes 0.
+ */
+#define SS_MOMENT_BLOCK 128
+#define SS_CHUNK_BYTES 32
+typedef struct {
+    int64_t numel;       /* >= 0 */
+    int32_t dtype;       /* of the parameter: SS_F32, SS_BF16 or SS_F16 */
+    int32_t grad_dtype;  /* that type, or SS_F32 */
+    int32_t no_decay;    /* 1: weight decay leaves the tensor out */
+    int32_t reserved;    /* 0 */
+} ss_tensor;
+typedef struct {
+    int32_t num_tensors;
+    int32_t num_chunks;
+    int64_t state_elems;
+    const void *chunks;  /* device */
+} ss_tensor_list;
+int32_t ss_tensor_list_plan(const ss_tensor *tensors, int32_t n, ss_tensor_list *list,
+                            void *chunks, size_t chunks_bytes);
+
+/*
+ * Norm of all gradients together, and the factor that clips them:
+ *     norm   = |grad_scale| * sqrt( sum over all elements of grad^2 )       (summed in fp64)
+ *     factor = grad_scale * min(1, max_norm / (norm + 1e-6)),  0 if norm is not finite
+ *   grads       device array of list->num_tensors device pointers, each of the list's grad_dtype
+ *   max_norm    > 0; +inf: nothing is clipped, factor = grad_scale
+ *   grad_scale  what the gradients are to be multiplied by before anything else (the inverse of a
+ *               loss scale; 1)
+ *   clip        device float[4], 16-byte aligned: norm, factor, 1 if norm is finite else 0, 0
+ *   ws          device workspace of ss_grad_norm_workspace_bytes(list) bytes, 256-byte aligned
+ * The sum has a fixed order: equal inputs give equal bits.  Two calls whose work may overlap need
+ * a workspace each.
+ */
+size_t ss_grad_norm_workspace_bytes(const ss_tensor_list *list);
+int32_t ss_grad_norm(const ss_tensor_list *list, const void *const *grads, double max_norm,
+                     double grad_scale, float *clip, void *ws, size_t ws_bytes, void *stream);
+
+/*
+ * One step of AdamW over all tensors of a list.  With f = clip[1] (1 without clip) and t the
+ * number of this step (1 for the first):
+ *     g = f * grad
+ *     m = beta1 * m + (1 - beta1) * g
+ *     v = beta2 * v + (1 - beta2) * g^2
+ *     p = p * (1 - lr * weight_decay) - lr / (1 - beta1^t) * m / (sqrt(v / (1 - beta2^t)) + eps)
+ * in fp32.  Where clip[2] is 0 (a norm that is not finite) nothing changes but the count of steps
+ * left out.  A 16-bit parameter with a master copy is the copy rounded to nearest; without one its
+ * own value is read, and the result rounded to nearest.
+ *
+ * ss_adamw_state (the struct is host memory, what it points to device memory of the caller's):
+ *   bits      32: m and v are float [state_elems]
+ *             8: m and v are uint8 [state_elems], exps is uint8 [state_elems / SS_MOMENT_BLOCK][2];
+ *             see below
+ *   master    float [state_elems] or NULL; used for the tensors of 16 bits
+ *   counters  64 bytes, 64-byte aligned, zeroed before the first step: int64 steps taken, int64
+ *             steps left out, and the scalars of the step in progress.  A step counts itself on
+ *             the device, so that it can be captured in a graph and replayed.
+ * m, v, exps and master are 16-byte aligned.  All zeros is the state before the first step, in
+ * either form.
+ *
+ * ss_adamw_hyper (host memory, read before the call returns): lr, weight_decay >= 0 and finite,
+ * 0 <= beta < 1, 1e-30 <= eps, all finite.  lr_device: NULL, or a device float that is read instead
+ * of lr when the step runs (a schedule for a captured step).
+ *
+ *   params    device array of num_tensors device pointers
+ *   grads     device array of num_tensors device pointers, read only
+ *   clip      device float[4] as ss_grad_norm writes it, or NULL
+ *
+ * Moments in 8 bits.  The elements of a tensor are taken in blocks of SS_MOMENT_BLOCK; exps holds
+ * a byte b for m and one for v per block: the exponent field of the block's largest |m| as an fp32
+ * number, at least 14, and of its largest v, at least 30.  The code of m is a sign and the upper
+ * bits (from bit 20 on) of the fp32 number |m| * 2^(14 - b): 4 exponent and 3 mantissa bits; that
+ * of v the upper bits of v * 2^(30 - b): 5 and 3.  Which neighbour a value is rounded to is decided
+ * by the 20 bits below, compared with a dither of element and step (element i of the state arrays,
+ * step t: the upper 20 bits of u = i * 0x6A09E667 + h(t) mod 2^32, for v of u + 2^31; h(t): h = t *
+ * 0x9E3779B9, h = (h ^ h >> 15) * 0x6A09E667, h = (h ^ h >> 13) * 0x9E3779B9, h ^ h >> 16):
+ * over the steps each element is rounded up as often as its value asks for, where rounding to
+ * the nearest would leave v as it is (it moves by 0.1 % of itself a step, codes are 6 to 12 %
+ * apart).  A v > 0 never becomes 0.  An element whose new v is not finite is left out of its block's
+ * exponents and stored as m = 0 and v = code 255.  The parameters' step uses the moments before
+ * they are rounded.
+ * ss_adamw_moments writes the values that 8-bit moments stand for, which bf16 holds exactly, into
+ * device arrays of state_elems elements (16-byte aligned; NULL: not wanted).
+ */
+typedef struct {
+    int32_t bits;
+    int32_t reserved;    /* 0 */
+    void *m;
+    void *v;
+    uint8_t *exps;
+    float *master;
+    void *counters;
+} ss_adamw_state;
+typedef struct {
+    double lr, beta1, beta2, eps, weight_decay;
+    const float *lr_device;
+} ss_adamw_hyper;
+int32_t ss_adamw_step(const ss_tensor_list *list, void *const *params, const void *const *grads,
+                      const ss_adamw_state *state, const ss_adamw_hyper *hyper,
+                      const float *clip, void *stream);
+int32_t ss_adamw_moments(const ss_tensor_list *list, const ss_adamw_state *state, void *m_bf,
+                         void *v_bf, void *stream);
+
+/*
+ * Layer normalization of the rows of a matrix: the dense vectors of section 3.5 (ss_layernorm_*
+ * takes the pooled ones).  Formulas as there, one gamma and beta for all rows; the statistics
+ * are fp32, sums are taken in fp32.
+ *   dtype        of x, y, dy and dx: SS_F32, SS_BF16 or SS_F16
+ *   param_dtype  of gamma, beta, dgamma and dbeta: dtype or SS_F32
+ *   rows >= 0, 1 <= dim <= 1048576; row r of a matrix starts at element r * its stride (>= dim,
+ *                in elements); matrices start at any address their type allows.  What lies between
+ *                the rows is neither read nor written.
+ *   n_valid      device int32 in [0, rows] or NULL: rows from it on are neither read nor written
+ *   gamma, beta  device [dim], or NULL for 1 and 0
+ *   mean, rstd   device fp32 [rows]
+ *   y may be x itself (same stride), dx may be dy or x.
+ * dgamma / dbeta (device [dim], NULL: not wanted): sums over the valid rows in a fixed order, 0
+ * where there is none.  If one is given, ws holds ss_layernorm_rows_workspace_bytes(rows, dim)
+ * bytes, 256-byte aligned (the size falls in neither argument).
+ */
+int32_t ss_layernorm_rows_forward(int32_t dtype, int32_t param_dtype, int32_t rows, int32_t dim,
+                                  const void *x, int64_t x_stride, const int32_t *n_valid,
+                                  const void *gamma, const void *beta, float eps, void *y,
+                                  int64_t y_stride, float *mean, float *rstd, void *stream);
+size_t ss_layernorm_rows_workspace_bytes(int32_t rows, int32_t dim);
+int32_t ss_layernorm_rows_backward(int32_t dtype, int32_t param_dtype, int32_t rows, int32_t dim,
+                                   const void *dy, int64_t dy_stride, const void *x,
+                                   int64_t x_stride, const int32_t *n_valid, const void *gamma,
+                                   const float *mean, const float *rstd, void *dx,
+                                   int64_t dx_stride, void *dgamma, void *dbeta, void *ws,
+                                   size_t ws_bytes, void *stream);
+
+/*
  * Issue queue: a host thread of the library's own that enqueues work on HIP
  * streams, for callers whose single host thread cannot enqueue a batch as fast
  * as the GPU finishes it (enqueueing one kernel costs the host about 3 us here;

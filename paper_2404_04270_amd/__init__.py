@@ -21,16 +21,19 @@ _BINDING_NAMES = (
     "ss_embbag_backward_update_noalloc", "ss_filter_batch_split", "ss_check_enable",
     "ss_check_indices", "ss_step_plan_for", "ss_step_create", "ss_step_destroy",
     "ss_step_room", "ss_step_submit", "ss_step_forward", "ss_step_backward", "ss_step_flush",
-    "EmbeddingStep", "PipelinedStep", "lib_path",
+    "TensorList", "AdamWState", "ss_grad_norm", "ss_grad_norm_workspace_bytes", "ss_adamw_step",
+    "ss_adamw_moments", "ss_layernorm_rows_forward", "ss_layernorm_rows_backward",
+    "ss_layernorm_rows_workspace_bytes",
+    "EmbeddingStep", "PipelinedStep", "AdamW", "lib_path",
 )
+_MODULE_OF = {"EmbeddingStep": "step", "PipelinedStep": "step", "AdamW": "optim"}
 
 
 def __getattr__(name):
-    if name in _BINDING_NAMES or name in ("binding", "step"):
+    if name in _BINDING_NAMES or name in ("binding", "step", "optim"):
         import importlib
-        if name in ("step", "EmbeddingStep", "PipelinedStep"):
-            mod = importlib.import_module(".step", __name__)
-            return mod if name == "step" else getattr(mod, name)
-        mod = importlib.import_module(".binding", __name__)
-        return mod if name == "binding" else getattr(mod, name)
+        if name in ("binding", "step", "optim"):
+            return importlib.import_module("." + name, __name__)
+        mod = importlib.import_module("." + _MODULE_OF.get(name, "binding"), __name__)
+        return getattr(mod, name)
     raise AttributeError(name)

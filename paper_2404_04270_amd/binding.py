@@ -34,7 +34,9 @@ SYMBOLS = (
     "ss_step_submit", "ss_step_forward", "ss_step_backward", "ss_step_flush",
     "ss_step_create_traced", "ss_filter_batch_split", "ss_profile_trace",
     "ss_step_counters", "ss_pointer_table", "ss_sample_levels", "ss_level_counts",
-    "ss_drop_stats_many",
+    "ss_drop_stats_many", "ss_tensor_list_plan", "ss_grad_norm_workspace_bytes", "ss_grad_norm",
+    "ss_adamw_step", "ss_adamw_moments", "ss_layernorm_rows_forward",
+    "ss_layernorm_rows_workspace_bytes", "ss_layernorm_rows_backward",
 )
 
 
@@ -48,10 +50,32 @@ class _CTables(C.Structure):
                 ("stale_bits", C.c_void_p)]
 
 
+class _CTensor(C.Structure):
+    _fields_ = [("numel", C.c_int64), ("dtype", C.c_int32), ("grad_dtype", C.c_int32),
+                ("no_decay", C.c_int32), ("reserved", C.c_int32)]
+
+
+class _CTensorList(C.Structure):
+    _fields_ = [("num_tensors", C.c_int32), ("num_chunks", C.c_int32),
+                ("state_elems", C.c_int64), ("chunks", C.c_void_p)]
+
+
+class _CAdamWState(C.Structure):
+    _fields_ = [("bits", C.c_int32), ("reserved", C.c_int32), ("m", C.c_void_p),
+                ("v", C.c_void_p), ("exps", C.c_void_p), ("master", C.c_void_p),
+                ("counters", C.c_void_p)]
+
+
+class _CAdamWHyper(C.Structure):
+    _fields_ = [("lr", C.c_double), ("beta1", C.c_double), ("beta2", C.c_double),
+                ("eps", C.c_double), ("weight_decay", C.c_double), ("lr_device", C.c_void_p)]
+
+
 # Argument types of the calls a training or preprocessing loop makes: with them ctypes takes plain
 # numbers and addresses, which costs less than an object of its own per argument.
-# t: ss_tables *, p: address, i / l: int32 / int64, f / d: float / double, z: size
-_ARG = {"t": C.POINTER(_CTables), "p": C.c_void_p, "i": C.c_int32, "l": C.c_int64,
+# t: ss_tables *, n: ss_tensor_list *, a: ss_adamw_state *, h: ss_adamw_hyper *, p: address, i / l: int32 / int64, f / d: float / double, z: size
+_ARG = {"t": C.POINTER(_CTables), "n": C.POINTER(_CTensorList), "a": C.POINTER(_CAdamWState),
+        "h": C.POINTER(_CAdamWHyper), "p": C.c_void_p, "i": C.c_int32, "l": C.c_int64,
         "f": C.c_float, "d": C.c_double, "z": C.c_size_t}
 _SIGNATURES = {
     "ss_filter_batch": "tpiiipppppzp",
@@ -74,6 +98,14 @@ _SIGNATURES = {
     "ss_sample_levels": "ipippiipp",
     "ss_level_counts": "pipipp",
     "ss_drop_stats_many": "pilll" "dp",
+    "ss_tensor_list_plan": "pinpz",
+    "ss_grad_norm_workspace_bytes": "n",
+    "ss_grad_norm": "npddppzp",
+    "ss_adamw_step": "nppahpp",
+    "ss_adamw_moments": "nappp",
+    "ss_layernorm_rows_forward": "iiiiplpppfplppp",
+    "ss_layernorm_rows_workspace_bytes": "ii",
+    "ss_layernorm_rows_backward": "iiiiplplppp" "pplppp" "zp",
 }
 
 
@@ -89,6 +121,8 @@ def _load():
     lib.ss_backward_workspace_bytes.restype = C.c_size_t
     lib.ss_select_hot_workspace_bytes.restype = C.c_size_t
     lib.ss_layernorm_backward_workspace_bytes.restype = C.c_size_t
+    lib.ss_grad_norm_workspace_bytes.restype = C.c_size_t
+    lib.ss_layernorm_rows_workspace_bytes.restype = C.c_size_t
     lib.ss_profile_enable.restype = None
     for n in ("ss_filter_batch", "ss_embbag_forward",
               "ss_embbag_backward_update", "ss_detect_stale",
@@ -105,7 +139,9 @@ def _load():
               "ss_step_room", "ss_step_submit", "ss_step_forward", "ss_step_backward",
               "ss_step_flush", "ss_step_create_traced", "ss_filter_batch_split",
               "ss_profile_trace", "ss_step_counters", "ss_pointer_table",
-              "ss_sample_levels", "ss_level_counts", "ss_drop_stats_many"):
+              "ss_sample_levels", "ss_level_counts", "ss_drop_stats_many", "ss_tensor_list_plan",
+              "ss_grad_norm", "ss_adamw_step", "ss_adamw_moments", "ss_layernorm_rows_forward",
+              "ss_layernorm_rows_backward"):
         getattr(lib, n).restype = C.c_int32
     lib.ss_check_enable.restype = None
     for name, sig in _SIGNATURES.items():
@@ -741,6 +777,258 @@ def ss_embbag_ln_backward(tables: Tables, idx: torch.Tensor, n_valid: Optional[t
         _ptr(rstd, torch.float32, "rstd"), _ptr(dx, torch.float32, "dx"),
         _ptr(dgamma, torch.float32, "dgamma"), _ptr(dbeta, torch.float32, "dbeta"),
         _ptr(ws, torch.uint8, "ws"), 0 if ws is None else ws.numel(),
+        _stream_ptr(stream)))
+
+
+DTYPES = {torch.float32: 0, torch.bfloat16: 1, torch.float16: 2}
+MOMENT_BLOCK = 128
+
+
+def _here(device: torch.device, who: str) -> None:
+    """The library launches on the current device: tensors of another one are refused."""
+    if torch.cuda.current_device() != device.index:
+        raise SlipstreamError(f"{who}: the tensors are on {device}, which is not the current "
+                              "device")
+
+
+class TensorList:
+    """The tensors of a model (contiguous, fp32 / bf16 / fp16, views at any place of a buffer among
+    them), with the work table and the pointer arrays that ss_grad_norm and ss_adamw_step read.
+
+    grads: the gradients, each of its parameter's shape and of its type or fp32; grad_dtypes alone
+    leaves them to set_grads.  With neither, the tensors are taken for gradients themselves (a
+    list for ss_grad_norm).  no_decay: truth values, one per tensor.
+    The work table and a first pointer array are copied here, with the host waiting."""
+
+    def __init__(self, params: Sequence[torch.Tensor],
+                 grads: Optional[Sequence[torch.Tensor]] = None,
+                 grad_dtypes: Optional[Sequence[torch.dtype]] = None,
+                 no_decay: Optional[Sequence[bool]] = None):
+        self.params: List[torch.Tensor] = list(params)
+        n = len(self.params)
+        if n == 0:
+            raise SlipstreamError("TensorList: no tensors")
+        self.device = self.params[0].device
+        for p in self.params:
+            if p.dtype not in DTYPES:
+                raise SlipstreamError(f"TensorList: {p.dtype} is not one of fp32, bf16, fp16")
+            _dev_ptr(p, p.dtype, "params")
+            if p.device != self.device:
+                raise SlipstreamError("TensorList: the tensors are on several devices")
+        if grads is None and grad_dtypes is None:
+            grads = self.params
+        if grad_dtypes is None:
+            grad_dtypes = [g.dtype for g in grads]
+        self.grad_dtypes = list(grad_dtypes)
+        no_decay = [False] * n if no_decay is None else list(no_decay)
+        if len(self.grad_dtypes) != n or len(no_decay) != n:
+            raise SlipstreamError("TensorList: one gradient type and one no_decay per tensor")
+        for p, d in zip(self.params, self.grad_dtypes):
+            if d not in (p.dtype, torch.float32):
+                raise SlipstreamError(f"TensorList: gradients of {d} for a parameter of {p.dtype}")
+        tensors = (_CTensor * n)(*[
+            (p.numel(), DTYPES[p.dtype], DTYPES[d], int(bool(k)), 0)
+            for p, d, k in zip(self.params, self.grad_dtypes, no_decay)])
+        self.c = _CTensorList()
+        _check(_lib.ss_tensor_list_plan(tensors, n, self.c, None, 0))
+        table = torch.empty(max(1, self.c.num_chunks) * 32, dtype=torch.uint8)
+        _check(_lib.ss_tensor_list_plan(tensors, n, self.c, table.data_ptr(), table.numel()))
+        self._chunks = table.to(self.device)
+        self.c.chunks = self._chunks.data_ptr()
+        self.state_elems = int(self.c.state_elems)
+        starts, at = [], 0
+        for p in self.params:
+            starts.append(at)
+            at += -(-p.numel() // MOMENT_BLOCK) * MOMENT_BLOCK
+        self.starts = starts
+        self._pptr = _ptr_table(self.params, self.device)
+        self.grads: Optional[List[torch.Tensor]] = None
+        self._gptr: Optional[torch.Tensor] = None
+        if grads is not None:
+            self._check_grads(list(grads))
+            self.grads = list(grads)
+            self._gptr = _ptr_table(self.grads, self.device)
+
+    def _check_grads(self, grads) -> List[int]:
+        if len(grads) != len(self.params):
+            raise SlipstreamError("grads: one per tensor")
+        for g, p, d in zip(grads, self.params, self.grad_dtypes):
+            if g.dtype is not d or g.numel() != p.numel() or g.device != self.device \
+                    or not g.is_contiguous():
+                raise SlipstreamError(
+                    f"grads: need {d}, contiguous, {p.numel()} elements on {self.device}")
+        return [g.data_ptr() for g in grads]
+
+    def set_grads(self, grads: Sequence[torch.Tensor], stream=None) -> None:
+        """The gradients that the calls after this one read, in order on the stream.  Under capture
+        the addresses become part of the graph."""
+        _here(self.device, "set_grads")
+        ptrs = self._check_grads(grads)
+        if self._gptr is None:
+            self._gptr = torch.zeros(len(ptrs), dtype=torch.int64, device=self.device)
+        ss_pointer_table(self._gptr, ptrs, stream)
+        self.grads = list(grads)
+
+    def of(self, flat: torch.Tensor, k: int) -> torch.Tensor:
+        """Tensor k's part of an array of state_elems elements."""
+        return flat[self.starts[k]:self.starts[k] + self.params[k].numel()]
+
+
+def ss_tensor_list_plan(params, grads=None, grad_dtypes=None, no_decay=None) -> TensorList:
+    return TensorList(params, grads, grad_dtypes, no_decay)
+
+
+def ss_grad_norm_workspace_bytes(tensors: TensorList) -> int:
+    return int(_lib.ss_grad_norm_workspace_bytes(tensors.c))
+
+
+def ss_grad_norm(tensors: TensorList, max_norm: float, clip: torch.Tensor, ws: torch.Tensor,
+                 grad_scale: float = 1.0, stream=None) -> None:
+    """clip fp32 [4]: norm, clip factor, 1 where the norm is finite, 0."""
+    _here(tensors.device, "ss_grad_norm")
+    if tensors._gptr is None:
+        raise SlipstreamError("ss_grad_norm: the list has no gradients yet (set_grads)")
+    if clip.numel() < 4:
+        raise SlipstreamError("ss_grad_norm: clip needs four floats")
+    _check(_lib.ss_grad_norm(
+        tensors.c, tensors._gptr.data_ptr(), max_norm, grad_scale,
+        _ptr(clip, torch.float32, "clip"), _ptr(ws, torch.uint8, "ws"), ws.numel(),
+        _stream_ptr(stream)))
+
+
+class AdamWState:
+    """Moments of a list's tensors in 32 or in 8 bits, fp32 copies of its 16-bit parameters if
+    asked for, and the step's counters: zeros before the first step, made on the current stream.
+    Arrays hold the tensors one after the other, each padded to MOMENT_BLOCK elements
+    (TensorList.of cuts one out)."""
+
+    def __init__(self, tensors: TensorList, bits: int = 32, master: bool = False):
+        if bits not in (32, 8):
+            raise SlipstreamError("AdamWState: moments are held in 32 or in 8 bits")
+        n, dev = tensors.state_elems, tensors.device
+        dt = torch.float32 if bits == 32 else torch.uint8
+        self.bits = bits
+        self.m = torch.zeros(n, dtype=dt, device=dev)
+        self.v = torch.zeros(n, dtype=dt, device=dev)
+        self.exps = (torch.zeros(n // MOMENT_BLOCK, 2, dtype=torch.uint8, device=dev)
+                     if bits == 8 else None)
+        self.master = None
+        if master:
+            self.master = torch.zeros(n, device=dev)
+            for k, p in enumerate(tensors.params):
+                tensors.of(self.master, k).copy_(p.detach().reshape(-1))
+        self.counters = torch.zeros(8, dtype=torch.int64, device=dev)
+        self.c = _CAdamWState(
+            bits, 0, self.m.data_ptr(), self.v.data_ptr(),
+            None if self.exps is None else self.exps.data_ptr(),
+            None if self.master is None else self.master.data_ptr(), self.counters.data_ptr())
+
+
+def ss_adamw_step(tensors: TensorList, state: AdamWState, lr, beta1: float = 0.9,
+                  beta2: float = 0.999, eps: float = 1e-8, weight_decay: float = 0.01,
+                  clip: Optional[torch.Tensor] = None, stream=None) -> None:
+    """lr: a number, or a device tensor of one float that is read when the step runs."""
+    _here(tensors.device, "ss_adamw_step")
+    if tensors._gptr is None:
+        raise SlipstreamError("ss_adamw_step: the list has no gradients yet (set_grads)")
+    if state.m.numel() != tensors.state_elems:
+        raise SlipstreamError("ss_adamw_step: the state belongs to another list")
+    if clip is not None and clip.numel() < 4:
+        raise SlipstreamError("ss_adamw_step: clip needs four floats")
+    at = None
+    if isinstance(lr, torch.Tensor):
+        if lr.numel() != 1:
+            raise SlipstreamError("ss_adamw_step: lr needs one float")
+        lr, at = 0.0, _ptr(lr, torch.float32, "lr")
+    _check(_lib.ss_adamw_step(
+        tensors.c, tensors._pptr.data_ptr(), tensors._gptr.data_ptr(), state.c,
+        _CAdamWHyper(lr, beta1, beta2, eps, weight_decay, at), _ptr(clip, torch.float32, "clip"),
+        _stream_ptr(stream)))
+
+
+def ss_adamw_moments(tensors: TensorList, state: AdamWState, m: Optional[torch.Tensor],
+                     v: Optional[torch.Tensor], stream=None) -> None:
+    """m, v bf16 [state_elems]: the values that 8-bit moments stand for."""
+    _here(tensors.device, "ss_adamw_moments")
+    for out in (m, v):
+        if out is not None and out.numel() < state.m.numel():
+            raise SlipstreamError("ss_adamw_moments: an output is too small")
+    if state.m.numel() != tensors.state_elems:
+        raise SlipstreamError("ss_adamw_moments: the state belongs to another list")
+    _check(_lib.ss_adamw_moments(
+        tensors.c, state.c, _ptr(m, torch.bfloat16, "m"), _ptr(v, torch.bfloat16, "v"),
+        _stream_ptr(stream)))
+
+
+def _rows(x: torch.Tensor, name: str):
+    """Address and row stride of a matrix whose rows are contiguous."""
+    if x.dim() != 2:
+        raise SlipstreamError(f"{name}: need [rows, dim]")
+    if not x.is_cuda:
+        raise SlipstreamError(f"{name}: need a device tensor")
+    if x.shape[1] > 1 and x.stride(1) != 1:
+        raise SlipstreamError(f"{name}: need contiguous rows")
+    if x.shape[0] > 1 and x.stride(0) < x.shape[1]:
+        raise SlipstreamError(f"{name}: rows overlap")
+    return x.data_ptr(), x.stride(0) if x.shape[0] > 1 else x.shape[1]
+
+
+def _rows_types(who: str, x: torch.Tensor, params, *same):
+    _here(x.device, who)
+    if x.dtype not in DTYPES:
+        raise SlipstreamError(f"{who}: {x.dtype} is not one of fp32, bf16, fp16")
+    for t in same:
+        if t.shape != x.shape or t.dtype != x.dtype or t.device != x.device:
+            raise SlipstreamError(f"{who}: matrices need one shape, type and device")
+    given = [p for p in params if p is not None]
+    wt = given[0].dtype if given else x.dtype
+    if wt not in (x.dtype, torch.float32) or any(p.dtype != wt for p in given):
+        raise SlipstreamError(f"{who}: parameters and their gradients need one type, "
+                              f"{x.dtype} or fp32")
+    if any(p.numel() != x.shape[1] or p.device != x.device for p in given):
+        raise SlipstreamError(f"{who}: parameters need one element per column")
+    return DTYPES[x.dtype], DTYPES[wt], wt
+
+
+def ss_layernorm_rows_forward(x: torch.Tensor, n_valid: Optional[torch.Tensor],
+                              gamma: Optional[torch.Tensor], beta: Optional[torch.Tensor],
+                              eps: float, y: torch.Tensor, mean: torch.Tensor,
+                              rstd: torch.Tensor, stream=None) -> None:
+    """x, y [rows, dim] (rows may be a stride apart); gamma, beta [dim]; mean, rstd fp32 [rows]."""
+    xp, xs = _rows(x, "x")
+    yp, ys = _rows(y, "y")
+    dt, pt, wt = _rows_types("ss_layernorm_rows_forward", x, (gamma, beta), y)
+    rows, dim = x.shape
+    if mean.numel() < rows or rstd.numel() < rows:
+        raise SlipstreamError("ss_layernorm_rows_forward: mean or rstd is too small")
+    _check(_lib.ss_layernorm_rows_forward(
+        dt, pt, rows, dim, xp, xs, _ptr(n_valid, torch.int32, "n_valid"),
+        _ptr(gamma, wt, "gamma"), _ptr(beta, wt, "beta"), eps, yp, ys,
+        _ptr(mean, torch.float32, "mean"), _ptr(rstd, torch.float32, "rstd"),
+        _stream_ptr(stream)))
+
+
+def ss_layernorm_rows_workspace_bytes(rows: int, dim: int) -> int:
+    return int(_lib.ss_layernorm_rows_workspace_bytes(rows, dim))
+
+
+def ss_layernorm_rows_backward(dy: torch.Tensor, x: torch.Tensor,
+                               n_valid: Optional[torch.Tensor], gamma: Optional[torch.Tensor],
+                               mean: torch.Tensor, rstd: torch.Tensor, dx: torch.Tensor,
+                               dgamma: Optional[torch.Tensor], dbeta: Optional[torch.Tensor],
+                               ws: Optional[torch.Tensor], stream=None) -> None:
+    dyp, dys = _rows(dy, "dy")
+    xp, xs = _rows(x, "x")
+    dxp, dxs = _rows(dx, "dx")
+    dt, pt, wt = _rows_types("ss_layernorm_rows_backward", x, (gamma, dgamma, dbeta), dy, dx)
+    rows, dim = x.shape
+    if mean.numel() < rows or rstd.numel() < rows:
+        raise SlipstreamError("ss_layernorm_rows_backward: mean or rstd is too small")
+    _check(_lib.ss_layernorm_rows_backward(
+        dt, pt, rows, dim, dyp, dys, xp, xs, _ptr(n_valid, torch.int32, "n_valid"),
+        _ptr(gamma, wt, "gamma"), _ptr(mean, torch.float32, "mean"),
+        _ptr(rstd, torch.float32, "rstd"), dxp, dxs, _ptr(dgamma, wt, "dgamma"),
+        _ptr(dbeta, wt, "dbeta"), _ptr(ws, torch.uint8, "ws"), 0 if ws is None else ws.numel(),
         _stream_ptr(stream)))
 
 
