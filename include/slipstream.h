@@ -452,8 +452,8 @@ enum { SS_F32 = 0, SS_BF16 = 1, SS_F16 = 2 };
  * ss_tensor_list_plan (host arithmetic only) sets num_tensors, num_chunks and state_elems of *list
  * (list->chunks is left alone) and, if `chunks` is not NULL, writes the num_chunks * SS_CHUNK_BYTES
  * bytes of the list's work table there.  The caller copies them to device memory (8-byte aligned)
- * and sets list->chunks to that copy; the table holds no address, only sizes and types.  A list
- * of up to 2^31 - 1 chunks (of 2048 elements at least) is taken.
+ * and sets list->chunks to that copy; the table holds no address, only sizes and types.  Lists of up
+ * to 2^24 - 1 chunks of 2048 elements (32 G elements) are taken.
  * Per-element arrays that go with a list (moments, master copies) hold the tensors one after the
  * other, each padded to a multiple of SS_MOMENT_BLOCK elements: state_elems in all, tensor k's at
  * sum_{j<k} round_up(numel_j, SS_MOMENT_BLOCK).  Padding stays as it was or becomes 0.
@@ -515,10 +515,9 @@ int32_t ss_grad_norm(const ss_tensor_list *list, const void *const *grads, doubl
  * m, v, exps and master are 16-byte aligned.  All zeros is the state before the first step, in
  * either form.
  *
- * ss_adamw_hyper (host memory, read before the call returns): lr, weight_decay >= 0 and finite,
- * 0 <= beta < 1, 1e-30 <= eps, all finite.  lr_device: NULL, or a device float that is read instead
- * of lr when the step runs (a schedule for a captured step).
- *
+ *   lr, weight_decay >= 0 and finite, 0 <= beta < 1, 1e-30 <= eps <= 1e30
+ *   lr_device NULL, or a device float that is read instead of lr when the step runs (a schedule for
+ *             a captured step)
  *   params    device array of num_tensors device pointers
  *   grads     device array of num_tensors device pointers, read only
  *   clip      device float[4] as ss_grad_norm writes it, or NULL
@@ -548,13 +547,10 @@ typedef struct {
     float *master;
     void *counters;
 } ss_adamw_state;
-typedef struct {
-    double lr, beta1, beta2, eps, weight_decay;
-    const float *lr_device;
-} ss_adamw_hyper;
 int32_t ss_adamw_step(const ss_tensor_list *list, void *const *params, const void *const *grads,
-                      const ss_adamw_state *state, const ss_adamw_hyper *hyper,
-                      const float *clip, void *stream);
+                      const ss_adamw_state *state, double lr, const float *lr_device, double beta1,
+                      double beta2, double eps, double weight_decay, const float *clip,
+                      void *stream);
 int32_t ss_adamw_moments(const ss_tensor_list *list, const ss_adamw_state *state, void *m_bf,
                          void *v_bf, void *stream);
 

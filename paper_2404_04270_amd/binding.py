@@ -66,16 +66,12 @@ class _CAdamWState(C.Structure):
                 ("counters", C.c_void_p)]
 
 
-class _CAdamWHyper(C.Structure):
-    _fields_ = [("lr", C.c_double), ("beta1", C.c_double), ("beta2", C.c_double),
-                ("eps", C.c_double), ("weight_decay", C.c_double), ("lr_device", C.c_void_p)]
-
-
 # Argument types of the calls a training or preprocessing loop makes: with them ctypes takes plain
 # numbers and addresses, which costs less than an object of its own per argument.
-# t: ss_tables *, n: ss_tensor_list *, a: ss_adamw_state *, h: ss_adamw_hyper *, p: address, i / l: int32 / int64, f / d: float / double, z: size
+# t: ss_tables *, n: ss_tensor_list *, a: ss_adamw_state *, p: address, i / l: int32 / int64,
+# f / d: float / double, z: size
 _ARG = {"t": C.POINTER(_CTables), "n": C.POINTER(_CTensorList), "a": C.POINTER(_CAdamWState),
-        "h": C.POINTER(_CAdamWHyper), "p": C.c_void_p, "i": C.c_int32, "l": C.c_int64,
+        "p": C.c_void_p, "i": C.c_int32, "l": C.c_int64,
         "f": C.c_float, "d": C.c_double, "z": C.c_size_t}
 _SIGNATURES = {
     "ss_filter_batch": "tpiiipppppzp",
@@ -101,7 +97,7 @@ _SIGNATURES = {
     "ss_tensor_list_plan": "pinpz",
     "ss_grad_norm_workspace_bytes": "n",
     "ss_grad_norm": "npddppzp",
-    "ss_adamw_step": "nppahpp",
+    "ss_adamw_step": "nppad" "pddddpp",
     "ss_adamw_moments": "nappp",
     "ss_layernorm_rows_forward": "iiiiplpppfplppp",
     "ss_layernorm_rows_workspace_bytes": "ii",
@@ -786,7 +782,7 @@ MOMENT_BLOCK = 128
 
 def _here(device: torch.device, who: str) -> None:
     """The library launches on the current device: tensors of another one are refused."""
-    if torch.cuda.current_device() != device.index:
+    if torch._C._cuda_getDevice() != device.index:
         raise SlipstreamError(f"{who}: the tensors are on {device}, which is not the current "
                               "device")
 
@@ -915,8 +911,8 @@ class AdamWState:
         self.master = None
         if master:
             self.master = torch.zeros(n, device=dev)
-            for k, p in enumerate(tensors.params):
-                tensors.of(self.master, k).copy_(p.detach().reshape(-1))
+            torch._foreach_copy_([tensors.of(self.master, k) for k in range(len(tensors.params))],
+                                 [p.detach().reshape(-1) for p in tensors.params])
         self.counters = torch.zeros(8, dtype=torch.int64, device=dev)
         self.c = _CAdamWState(
             bits, 0, self.m.data_ptr(), self.v.data_ptr(),
@@ -941,9 +937,8 @@ def ss_adamw_step(tensors: TensorList, state: AdamWState, lr, beta1: float = 0.9
             raise SlipstreamError("ss_adamw_step: lr needs one float")
         lr, at = 0.0, _ptr(lr, torch.float32, "lr")
     _check(_lib.ss_adamw_step(
-        tensors.c, tensors._pptr.data_ptr(), tensors._gptr.data_ptr(), state.c,
-        _CAdamWHyper(lr, beta1, beta2, eps, weight_decay, at), _ptr(clip, torch.float32, "clip"),
-        _stream_ptr(stream)))
+        tensors.c, tensors._pptr.data_ptr(), tensors._gptr.data_ptr(), state.c, lr, at, beta1,
+        beta2, eps, weight_decay, _ptr(clip, torch.float32, "clip"), _stream_ptr(stream)))
 
 
 def ss_adamw_moments(tensors: TensorList, state: AdamWState, m: Optional[torch.Tensor],
@@ -960,34 +955,42 @@ def ss_adamw_moments(tensors: TensorList, state: AdamWState, m: Optional[torch.T
         _stream_ptr(stream)))
 
 
-def _rows(x: torch.Tensor, name: str):
-    """Address and row stride of a matrix whose rows are contiguous."""
-    if x.dim() != 2:
-        raise SlipstreamError(f"{name}: need [rows, dim]")
-    if not x.is_cuda:
-        raise SlipstreamError(f"{name}: need a device tensor")
-    if x.shape[1] > 1 and x.stride(1) != 1:
-        raise SlipstreamError(f"{name}: need contiguous rows")
-    if x.shape[0] > 1 and x.stride(0) < x.shape[1]:
-        raise SlipstreamError(f"{name}: rows overlap")
-    return x.data_ptr(), x.stride(0) if x.shape[0] > 1 else x.shape[1]
+def _matrix(who: str, name: str, t: torch.Tensor, like: torch.Tensor, shape):
+    """Address and row stride of a matrix whose rows are contiguous; of like's type and device."""
+    if t.dtype is not like.dtype or t.shape != shape or t.get_device() != like.get_device():
+        raise SlipstreamError(f"{who}: {name}: matrices need one shape, type and device")
+    dim = shape[1]
+    if t.is_contiguous():
+        return t.data_ptr(), dim
+    across, along = t.stride()
+    if along != 1 and dim > 1 or across < dim and shape[0] > 1:
+        raise SlipstreamError(f"{who}: {name}: need contiguous rows that do not overlap")
+    return t.data_ptr(), across if shape[0] > 1 else dim
 
 
-def _rows_types(who: str, x: torch.Tensor, params, *same):
-    _here(x.device, who)
-    if x.dtype not in DTYPES:
-        raise SlipstreamError(f"{who}: {x.dtype} is not one of fp32, bf16, fp16")
-    for t in same:
-        if t.shape != x.shape or t.dtype != x.dtype or t.device != x.device:
-            raise SlipstreamError(f"{who}: matrices need one shape, type and device")
-    given = [p for p in params if p is not None]
-    wt = given[0].dtype if given else x.dtype
-    if wt not in (x.dtype, torch.float32) or any(p.dtype != wt for p in given):
-        raise SlipstreamError(f"{who}: parameters and their gradients need one type, "
-                              f"{x.dtype} or fp32")
-    if any(p.numel() != x.shape[1] or p.device != x.device for p in given):
-        raise SlipstreamError(f"{who}: parameters need one element per column")
-    return DTYPES[x.dtype], DTYPES[wt], wt
+def _rows_args(who: str, x: torch.Tensor, params, mean: torch.Tensor, rstd: torch.Tensor):
+    """Shape, and the types of the matrices and of the parameters (gammas, betas, gradients)."""
+    shape, dtype, device = x.shape, x.dtype, x.get_device()
+    if len(shape) != 2 or device < 0:
+        raise SlipstreamError(f"{who}: x must be a device tensor [rows, dim]")
+    if device != torch._C._cuda_getDevice():
+        raise SlipstreamError(f"{who}: x is on {x.device}, which is not the current device")
+    if dtype not in DTYPES:
+        raise SlipstreamError(f"{who}: {dtype} is not one of fp32, bf16, fp16")
+    rows, dim = shape
+    wt = None
+    for p in params:
+        if p is not None:
+            if wt is None:
+                wt = p.dtype
+                if wt is not dtype and wt is not torch.float32:
+                    raise SlipstreamError(f"{who}: parameters of {wt} (need {dtype} or fp32)")
+            if p.dtype is not wt or p.numel() != dim or p.get_device() != device:
+                raise SlipstreamError(f"{who}: parameters and their gradients need one type and "
+                                      "one element per column")
+    if mean.numel() < rows or rstd.numel() < rows:
+        raise SlipstreamError(f"{who}: mean or rstd is too small")
+    return shape, DTYPES[dtype], dtype if wt is None else wt
 
 
 def ss_layernorm_rows_forward(x: torch.Tensor, n_valid: Optional[torch.Tensor],
@@ -995,14 +998,12 @@ def ss_layernorm_rows_forward(x: torch.Tensor, n_valid: Optional[torch.Tensor],
                               eps: float, y: torch.Tensor, mean: torch.Tensor,
                               rstd: torch.Tensor, stream=None) -> None:
     """x, y [rows, dim] (rows may be a stride apart); gamma, beta [dim]; mean, rstd fp32 [rows]."""
-    xp, xs = _rows(x, "x")
-    yp, ys = _rows(y, "y")
-    dt, pt, wt = _rows_types("ss_layernorm_rows_forward", x, (gamma, beta), y)
-    rows, dim = x.shape
-    if mean.numel() < rows or rstd.numel() < rows:
-        raise SlipstreamError("ss_layernorm_rows_forward: mean or rstd is too small")
+    who = "ss_layernorm_rows_forward"
+    shape, dt, wt = _rows_args(who, x, (gamma, beta), mean, rstd)
+    xp, xs = _matrix(who, "x", x, x, shape)
+    yp, ys = _matrix(who, "y", y, x, shape)
     _check(_lib.ss_layernorm_rows_forward(
-        dt, pt, rows, dim, xp, xs, _ptr(n_valid, torch.int32, "n_valid"),
+        dt, DTYPES[wt], shape[0], shape[1], xp, xs, _ptr(n_valid, torch.int32, "n_valid"),
         _ptr(gamma, wt, "gamma"), _ptr(beta, wt, "beta"), eps, yp, ys,
         _ptr(mean, torch.float32, "mean"), _ptr(rstd, torch.float32, "rstd"),
         _stream_ptr(stream)))
@@ -1017,19 +1018,17 @@ def ss_layernorm_rows_backward(dy: torch.Tensor, x: torch.Tensor,
                                mean: torch.Tensor, rstd: torch.Tensor, dx: torch.Tensor,
                                dgamma: Optional[torch.Tensor], dbeta: Optional[torch.Tensor],
                                ws: Optional[torch.Tensor], stream=None) -> None:
-    dyp, dys = _rows(dy, "dy")
-    xp, xs = _rows(x, "x")
-    dxp, dxs = _rows(dx, "dx")
-    dt, pt, wt = _rows_types("ss_layernorm_rows_backward", x, (gamma, dgamma, dbeta), dy, dx)
-    rows, dim = x.shape
-    if mean.numel() < rows or rstd.numel() < rows:
-        raise SlipstreamError("ss_layernorm_rows_backward: mean or rstd is too small")
+    who = "ss_layernorm_rows_backward"
+    shape, dt, wt = _rows_args(who, x, (gamma, dgamma, dbeta), mean, rstd)
+    dyp, dys = _matrix(who, "dy", dy, x, shape)
+    xp, xs = _matrix(who, "x", x, x, shape)
+    dxp, dxs = _matrix(who, "dx", dx, x, shape)
     _check(_lib.ss_layernorm_rows_backward(
-        dt, pt, rows, dim, dyp, dys, xp, xs, _ptr(n_valid, torch.int32, "n_valid"),
-        _ptr(gamma, wt, "gamma"), _ptr(mean, torch.float32, "mean"),
-        _ptr(rstd, torch.float32, "rstd"), dxp, dxs, _ptr(dgamma, wt, "dgamma"),
-        _ptr(dbeta, wt, "dbeta"), _ptr(ws, torch.uint8, "ws"), 0 if ws is None else ws.numel(),
-        _stream_ptr(stream)))
+        dt, DTYPES[wt], shape[0], shape[1], dyp, dys, xp, xs,
+        _ptr(n_valid, torch.int32, "n_valid"), _ptr(gamma, wt, "gamma"),
+        _ptr(mean, torch.float32, "mean"), _ptr(rstd, torch.float32, "rstd"), dxp, dxs,
+        _ptr(dgamma, wt, "dgamma"), _ptr(dbeta, wt, "dbeta"), _ptr(ws, torch.uint8, "ws"),
+        0 if ws is None else ws.numel(), _stream_ptr(stream)))
 
 
 def stream_handle(stream=None) -> C.c_void_p:

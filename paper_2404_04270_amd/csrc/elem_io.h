@@ -19,12 +19,15 @@ template <int DT, int N> struct Raw {
     V v;
 };
 
-template <int DT, int N>
+// STREAM: past the caches, for data that nobody reads again before they have been replaced.
+template <int DT, int N, bool STREAM = false>
 __device__ __forceinline__ Raw<DT, N> load_raw(const void *base, int64_t i)
 {
     typedef Raw<DT, N> R;
     R r;
-    r.v = *(gptr<const typename R::VU>)((gptr<const typename R::E>)base + i);
+    const auto p = (gptr<const typename R::VU>)((gptr<const typename R::E>)base + i);
+    if constexpr (STREAM) r.v = __builtin_nontemporal_load(p);
+    else r.v = *p;
     return r;
 }
 
@@ -57,11 +60,13 @@ __device__ __forceinline__ Raw<DT, N> from_float(const float (&f)[N])
     return r;
 }
 
-template <int DT, int N>
+template <int DT, int N, bool STREAM = false>
 __device__ __forceinline__ void store_raw(void *base, int64_t i, const Raw<DT, N> &r)
 {
     typedef Raw<DT, N> R;
-    *(gptr<typename R::VU>)((gptr<typename R::E>)base + i) = r.v;
+    const auto p = (gptr<typename R::VU>)((gptr<typename R::E>)base + i);
+    if constexpr (STREAM) __builtin_nontemporal_store(r.v, p);
+    else *p = r.v;
 }
 
 template <int DT, int N>

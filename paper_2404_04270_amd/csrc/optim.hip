@@ -23,8 +23,21 @@ struct Chunk {
 };
 static_assert(sizeof(Chunk) == SS_CHUNK_BYTES, "the header says how large an entry is");
 
-constexpr int kPass = 2048;                // elements that a workgroup takes at a time
-constexpr int kChunk = 4 * kPass;
+// Elements that a workgroup takes: one round trip to memory with all of its loads in flight.  With
+// 4096 elements in two rounds a step over 2^28 fp32 elements takes 1394 instead of 1341 us, in one
+// round of twice the loads 1334 instead of 1296.
+constexpr int kChunk = 2048;
+constexpr int64_t kMostChunks = 0xFFFFFFFFLL / kWG;    // threads of a launch are counted in 32 bits
+// Workgroups run on the eight XCDs in turn.  Eight chunks next to each other go to the same XCD,
+// which then works on pieces of 64 KB: 1296 instead of 1341 us.
+constexpr int kRun = 8;
+
+__device__ __forceinline__ int64_t chunk_of_block()
+{
+    const unsigned b = blockIdx.x, group = b / (8 * kRun), w = b % (8 * kRun);
+    if ((group + 1) * (8 * kRun) > gridDim.x) return b;
+    return group * (8 * kRun) + w % 8 * kRun + w / 8;
+}
 
 __device__ __forceinline__ Chunk load_chunk(const void *chunks, int64_t c)
 {
@@ -32,29 +45,39 @@ __device__ __forceinline__ Chunk load_chunk(const void *chunks, int64_t c)
 }
 
 // ---- gradient norm ------------------------------------------------------------------------
-constexpr int kNormWgs = 2048;             // eight workgroups per compute unit
+// Four workgroups per compute unit, and past the caches: 2^29 bf16 elements 170 us, 2^28 fp32 161 (6.3
+// and 6.7 TB/s); with twice as many 196 to 229, with half as many 174 and 180, through the caches 177
+// and 177.
+constexpr int kNormWgs = 1024;
 constexpr int kFinalThreads = 1024;
 
+template <int G, int N>
+__device__ __forceinline__ void add_squares(const Raw<G, N> &r, double &sum)
+{
+    float f[N];
+    to_float(r, f);
+#pragma unroll
+    for (int k = 0; k < N; ++k) sum = fma((double)f[k], (double)f[k], sum);
+}
+
+// Sum of the squares of a wavefront's chunk, a lane's part.
 template <int G>
 __device__ __forceinline__ double chunk_squares(const void *g, const Chunk &c)
 {
-    constexpr int N = G == SS_F32 ? 4 : 8, U = G == SS_F32 ? 4 : 2;
+    constexpr int N = G == SS_F32 ? 4 : 8, U = kChunk / (64 * N);
+    const int lane = threadIdx.x % 64;
     double sum = 0.0;
-    for (int e0 = threadIdx.x * N; e0 < c.count; e0 += kWG * N * U) {
+    if (c.count == kChunk) {
         Raw<G, N> r[U];
 #pragma unroll
-        for (int u = 0; u < U; ++u) {
-            const int e = e0 + u * kWG * N;
-            if (e + N <= c.count) r[u] = load_raw<G, N>(g, c.first + e);
-            else r[u] = load_raw_part<G, N>(g, c.first + e, c.count - e);
-        }
+        for (int u = 0; u < U; ++u) r[u] = load_raw<G, N, true>(g, c.first + (u * 64 + lane) * N);
 #pragma unroll
-        for (int u = 0; u < U; ++u) {
-            float f[N];
-            to_float(r[u], f);
-#pragma unroll
-            for (int k = 0; k < N; ++k) sum = fma((double)f[k], (double)f[k], sum);
-        }
+        for (int u = 0; u < U; ++u) add_squares(r[u], sum);
+        return sum;
+    }
+    for (int e = lane * N; e < c.count; e += 64 * N) {
+        if (e + N <= c.count) add_squares(load_raw<G, N>(g, c.first + e), sum);
+        else add_squares(load_raw_part<G, N>(g, c.first + e, c.count - e), sum);
     }
     return sum;
 }
@@ -74,14 +97,28 @@ __device__ __forceinline__ double wg_sum(double v)
     return v;
 }
 
+// A wavefront takes a chunk at a time; the entry of its next one is fetched meanwhile.
 __global__ __launch_bounds__(kWG) void norm_partial_kernel(const void *chunks, int num_chunks,
                                                            const void *const *grads,
                                                            double *__restrict__ part)
 {
+    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64);
+    const int64_t step = (int64_t)gridDim.x * (kWG / 64);
+    int64_t i = (int64_t)blockIdx.x * (kWG / 64) + wave;
     double sum = 0.0;
-    for (int64_t i = blockIdx.x; i < num_chunks; i += gridDim.x) {
-        const Chunk c = load_chunk(chunks, i);
-        const void *g = grads[c.tensor];
+    Chunk next{};
+    const void *g_next = nullptr;
+    if (i < num_chunks) {
+        next = load_chunk(chunks, i);
+        g_next = grads[next.tensor];
+    }
+    for (; i < num_chunks; i += step) {
+        const Chunk c = next;
+        const void *g = g_next;
+        if (i + step < num_chunks) {
+            next = load_chunk(chunks, i + step);
+            g_next = grads[next.tensor];
+        }
         switch (c.kind >> 2 & 3) {
         case SS_F32: sum += chunk_squares<SS_F32>(g, c); break;
         case SS_BF16: sum += chunk_squares<SS_BF16>(g, c); break;
@@ -121,7 +158,8 @@ struct Scalars {
     float factor;              // of the gradients
     uint32_t dither;           // of element 0
     int32_t apply;
-    int32_t reserved[6];
+    uint32_t ended;            // workgroups of the present step that have ended
+    int32_t reserved[5];
 };
 static_assert(sizeof(Scalars) == 64, "the header says how large the counters are");
 
@@ -139,25 +177,76 @@ __device__ __forceinline__ uint32_t mixed(uint32_t t)
     return h ^ h >> 16;
 }
 
-__global__ __launch_bounds__(64) void adamw_begin_kernel(Scalars *__restrict__ s,
-                                                         const float *__restrict__ clip,
-                                                         const float *__restrict__ lr_device,
-                                                         double lr, double beta1, double beta2,
-                                                         double weight_decay)
+struct Begin {
+    double lr, log1, log2, weight_decay;       // log1, log2: of the betas
+    const float *lr_device, *clip;
+};
+
+// The scalars of the step that follows what *old counts.
+__device__ __forceinline__ Scalars begin_step(const Scalars *__restrict__ old, const Begin &b)
+{
+    Scalars s;
+    const double lr = b.lr_device ? (double)*b.lr_device : b.lr;
+    s.apply = !b.clip || b.clip[2] != 0.0f;
+    s.factor = b.clip ? b.clip[1] : 1.0f;
+    s.steps = old->steps + s.apply;
+    s.left_out = old->left_out + !s.apply;
+    // 1 - beta^t without the cancellation of a beta next to 1; a beta of 0 (log -inf) gives 1
+    s.size = (float)(lr / -expm1((double)s.steps * b.log1));
+    s.keep = (float)(1.0 - lr * b.weight_decay);
+    s.root = (float)(1.0 / sqrt(-expm1((double)s.steps * b.log2)));
+    s.dither = mixed((uint32_t)s.steps);
+    return s;
+}
+
+__global__ __launch_bounds__(64) void adamw_begin_kernel(Scalars *scalars, Begin b)
 {
     if (threadIdx.x != 0) return;
-    if (lr_device) lr = *lr_device;
-    const bool apply = !clip || clip[2] != 0.0f;
-    const int64_t t = s->steps + (apply ? 1 : 0);
-    s->steps = t;
-    if (!apply) s->left_out += 1;
-    s->apply = apply;
-    s->factor = clip ? clip[1] : 1.0f;
-    // 1 - beta^t without the cancellation of a beta next to 1; log(0) gives 1
-    s->size = (float)(lr / -expm1((double)t * log(beta1)));
-    s->keep = (float)(1.0 - lr * weight_decay);
-    s->root = (float)(1.0 / sqrt(-expm1((double)t * log(beta2))));
-    s->dither = mixed((uint32_t)t);
+    Scalars s = begin_step(scalars, b);
+    s.ended = 0;
+    *scalars = s;
+}
+
+// A step of few workgroups has one launch: each works out the scalars for itself, and the last to end
+// counts the step (nobody waits: all have read the count by then).  A workgroup's turn at the
+// counter that tells the last takes about 16 ns: us per fp32 step of 60 / 140 / 260 / 380 / 500 chunks in
+// one launch and in two 5.2 / 5.2 / 6.9 / 9.0 / 11.5 and 7.5 / 8.1 / 7.7 / 7.7 / 8.5 (packed moments
+// 4.9 / - / 7.0 / - / 10.0 and 7.2 / - / 7.8 / - / 7.7).
+constexpr int kSoloChunks = 288;
+
+__device__ __forceinline__ int32_t uniform(int32_t x) { return __builtin_amdgcn_readfirstlane(x); }
+__device__ __forceinline__ float uniform(float x) { return __int_as_float(uniform(__float_as_int(x))); }
+
+// The scalars of a solo step, from the first wavefront (it is the arithmetic in fp64 that takes time).
+__device__ __forceinline__ Scalars begin_solo(const Scalars *scalars, const Begin &b)
+{
+    __shared__ Scalars shared;
+    if (threadIdx.x < 64) {
+        const Scalars s = begin_step(scalars, b);
+        if (threadIdx.x == 0) shared = s;
+    }
+    __syncthreads();
+    Scalars s = shared;
+    s.size = uniform(s.size);
+    s.keep = uniform(s.keep);
+    s.root = uniform(s.root);
+    s.factor = uniform(s.factor);
+    s.dither = (uint32_t)uniform((int32_t)s.dither);
+    s.apply = uniform(s.apply);
+    return s;
+}
+
+__device__ __forceinline__ void end_solo(Scalars *scalars, const Scalars &s)
+{
+    __syncthreads();           // every wavefront has used the count it read
+    if (threadIdx.x != 0) return;
+    const unsigned before = __hip_atomic_fetch_add(&scalars->ended, 1u, __ATOMIC_RELAXED,
+                                                   __HIP_MEMORY_SCOPE_AGENT);
+    if (before + 1 == gridDim.x) {
+        scalars->steps = s.steps;
+        scalars->left_out = s.left_out;
+        scalars->ended = 0;
+    }
 }
 
 struct Betas {
@@ -187,65 +276,101 @@ template <int N> __device__ __forceinline__ void as_stored(float (&f)[N])
     for (int i = 0; i < N; ++i) asm("" : "+v"(f[i]));
 }
 
-// Elements [e, e + N) of a chunk, n of them there.
-template <int P, int G, bool MASTER, bool WHOLE>
-__device__ __forceinline__ void step_four(const Chunk &c, int e, int n, void *p, const void *g,
-                                          float *m, float *v, float *master, const Betas &k,
-                                          const Scalars &s, float keep)
+// Four elements of a chunk on their way: what a lane has asked for.
+template <int P, int G, bool MASTER> struct Four {
+    Raw<P, 4> p;
+    Raw<G, 4> g;
+    f4 m, v, w;                // w: the master copy
+};
+
+// How a chunk is read and written: through the caches, past them, or past them but for parameters
+// and gradients (whose accesses share cache lines where a tensor starts at an odd place).
+enum Flow { kCached, kStream, kStreamMoments };
+
+template <Flow F> __device__ __forceinline__ f4 load_moments(const float *p)
 {
-    constexpr int N = 4;
-    const int64_t at = c.first + e, st = c.state + e;
-    Raw<P, N> pr;
-    Raw<G, N> gr;
-    if (WHOLE) {
-        if (!MASTER) pr = load_raw<P, N>(p, at);
-        gr = load_raw<G, N>(g, at);
-    } else {
-        if (!MASTER) pr = load_raw_part<P, N>(p, at, n);
-        gr = load_raw_part<G, N>(g, at, n);
-    }
-    const f4 m4 = *(gptr<const f4>)(m + st), v4 = *(gptr<const f4>)(v + st);
-    float pf[N], gf[N], mf[N], vf[N];
-    if (MASTER) {
-        const f4 p4 = *(gptr<const f4>)(master + st);
-#pragma unroll
-        for (int i = 0; i < N; ++i) pf[i] = p4[i];
-    } else {
-        to_float(pr, pf);
-    }
-    to_float(gr, gf);
-    f4 mo, vo, po;
-#pragma unroll
-    for (int i = 0; i < N; ++i) {
-        mf[i] = m4[i];
-        vf[i] = v4[i];
-        if (!WHOLE && i >= n) gf[i] = mf[i] = vf[i] = pf[i] = 0.0f;
-        moments(gf[i] * s.factor, mf[i], vf[i], k);
-        pf[i] = stepped(pf[i], mf[i], vf[i], k, s, keep);
-        mo[i] = mf[i];
-        vo[i] = vf[i];
-        po[i] = pf[i];
-    }
-    *(gptr<f4>)(m + st) = mo;
-    *(gptr<f4>)(v + st) = vo;
-    if (MASTER) *(gptr<f4>)(master + st) = po;
-    if (MASTER) as_stored(pf);
-    const Raw<P, N> pw = from_float<P, N>(pf);
-    if (WHOLE) store_raw<P, N>(p, at, pw);
-    else store_raw_part<P, N>(p, at, pw, n);
+    if constexpr (F != kCached) return __builtin_nontemporal_load((gptr<const f4>)p);
+    return *(gptr<const f4>)p;
+}
+template <Flow F> __device__ __forceinline__ void store_moments(float *p, f4 v)
+{
+    if constexpr (F != kCached) __builtin_nontemporal_store(v, (gptr<f4>)p);
+    else *(gptr<f4>)p = v;
 }
 
-template <int P, int G, bool MASTER>
-__device__ __forceinline__ void step_chunk(const Chunk &c, void *p, const void *g, float *m,
-                                           float *v, float *master, const Betas &k,
+// Tensors and moments of a chunk; element e of it is p[first + e] and m[state + e].
+struct Places {
+    void *p;
+    const void *g;
+    float *m, *v, *master;
+    int64_t first, state;
+};
+
+template <Flow F, int P, int G, bool MASTER, bool WHOLE>
+__device__ __forceinline__ void ask_four(const Places &at, int e, int n, Four<P, G, MASTER> &q)
+{
+    if (WHOLE) {
+        if (!MASTER) q.p = load_raw<P, 4, F == kStream>(at.p, at.first + e);
+        q.g = load_raw<G, 4, F == kStream>(at.g, at.first + e);
+    } else {
+        if (!MASTER) q.p = load_raw_part<P, 4>(at.p, at.first + e, n);
+        q.g = load_raw_part<G, 4>(at.g, at.first + e, n);
+    }
+    q.m = load_moments<F>(at.m + at.state + e);
+    q.v = load_moments<F>(at.v + at.state + e);
+    if (MASTER) q.w = load_moments<F>(at.master + at.state + e);
+}
+
+template <Flow F, int P, int G, bool MASTER, bool WHOLE>
+__device__ __forceinline__ void step_four(const Places &at, int e, int n,
+                                          const Four<P, G, MASTER> &q, const Betas &k,
+                                          const Scalars &s, float keep)
+{
+    float p[4], g[4], m[4], v[4];
+    if (!MASTER) to_float(q.p, p);
+    to_float(q.g, g);
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        if (MASTER) p[i] = q.w[i];
+        m[i] = q.m[i];
+        v[i] = q.v[i];
+        if (!WHOLE && i >= n) g[i] = m[i] = v[i] = p[i] = 0.0f;      // padding becomes 0
+        moments(g[i] * s.factor, m[i], v[i], k);
+        p[i] = stepped(p[i], m[i], v[i], k, s, keep);
+    }
+    if (MASTER) as_stored(p);
+    store_moments<F>(at.m + at.state + e, f4{m[0], m[1], m[2], m[3]});
+    store_moments<F>(at.v + at.state + e, f4{v[0], v[1], v[2], v[3]});
+    if (MASTER) store_moments<F>(at.master + at.state + e, f4{p[0], p[1], p[2], p[3]});
+    const Raw<P, 4> out = from_float<P, 4>(p);
+    if (WHOLE) store_raw<P, 4, F == kStream>(at.p, at.first + e, out);
+    else store_raw_part<P, 4>(at.p, at.first + e, out, n);
+}
+
+template <Flow F, int P, int G, bool MASTER>
+__device__ __forceinline__ void step_chunk(const Places &at, int count, const Betas &k,
                                            const Scalars &s, float keep)
 {
-    constexpr int N = 4;
-    for (int e = threadIdx.x * N; e < c.count; e += kWG * N) {
-        if (e + N <= c.count)
-            step_four<P, G, MASTER, true>(c, e, N, p, g, m, v, master, k, s, keep);
-        else
-            step_four<P, G, MASTER, false>(c, e, c.count - e, p, g, m, v, master, k, s, keep);
+    constexpr int U = kChunk / (kWG * 4), kStep = kWG * 4;
+    int e = threadIdx.x * 4;
+    if (count == kChunk) {
+        Four<P, G, MASTER> q[U];
+#pragma unroll
+        for (int u = 0; u < U; ++u) ask_four<F, P, G, MASTER, true>(at, e + u * kStep, 4, q[u]);
+#pragma unroll
+        for (int u = 0; u < U; ++u)
+            step_four<F, P, G, MASTER, true>(at, e + u * kStep, 4, q[u], k, s, keep);
+        return;
+    }
+    for (; e < count; e += kStep) {
+        Four<P, G, MASTER> q;
+        if (e + 4 <= count) {
+            ask_four<F, P, G, MASTER, true>(at, e, 4, q);
+            step_four<F, P, G, MASTER, true>(at, e, 4, q, k, s, keep);
+        } else {
+            ask_four<F, P, G, MASTER, false>(at, e, count - e, q);
+            step_four<F, P, G, MASTER, false>(at, e, count - e, q, k, s, keep);
+        }
     }
 }
 
@@ -261,19 +386,40 @@ __device__ __forceinline__ void step_chunk(const Chunk &c, void *p, const void *
     if (with_master) { constexpr bool MASTER = true; __VA_ARGS__; }                           \
     else { constexpr bool MASTER = false; __VA_ARGS__; }
 
+// From this many elements on a step goes past the caches: parameters, gradients and moments have
+// been replaced there before the next step reads them.  us per step over 2 / 4 / 8 / 16 / 32 M fp32
+// elements, streamed and not, three models in turn: 13.3 / 22.4 / 40.3 / 75.7 / 147 and 12.0 / 20.0 /
+// 45.4 / 86.5 / 167; one model with nothing else between its steps: 12.0 / 20.8 / 39.4 / 75.5 / 146
+// and 10.0 / 19.9 / 35.5 / 69.8 / 170.
+constexpr int64_t kStreamElems = 8 << 20;
+
+template <bool STREAM, bool SOLO>
 __global__ __launch_bounds__(kWG) void adamw_kernel(const void *chunks, void *const *params,
                                                     const void *const *grads, float *m, float *v,
-                                                    float *master,
-                                                    const Scalars *__restrict__ scalars, Betas k)
+                                                    float *master, Scalars *scalars, Betas k,
+                                                    Begin b)
 {
-    const Scalars s = *scalars;
-    if (!s.apply) return;
-    const Chunk c = load_chunk(chunks, blockIdx.x);
-    void *p = params[c.tensor];
-    const void *g = grads[c.tensor];
+    const Chunk c = load_chunk(chunks, chunk_of_block());
+    const Scalars s = SOLO ? begin_solo(scalars, b) : *scalars;
+    const Places at{params[c.tensor], grads[c.tensor], m, v, master, c.first, c.state};
     const float keep = c.kind & 16 ? 1.0f : s.keep;
-    SS_DISPATCH_KIND(c.kind, master != nullptr,
-                     step_chunk<P, G, MASTER>(c, p, g, m, v, master, k, s, keep));
+    if (!s.apply) {
+        if (SOLO) end_solo(scalars, s);
+        return;
+    }
+    const bool even = ((reinterpret_cast<uintptr_t>(at.p) | reinterpret_cast<uintptr_t>(at.g)) &
+                       15) == 0;
+    if (!STREAM) {
+        SS_DISPATCH_KIND(c.kind, master != nullptr,
+                         step_chunk<kCached, P, G, MASTER>(at, c.count, k, s, keep));
+    } else if (even) {
+        SS_DISPATCH_KIND(c.kind, master != nullptr,
+                         step_chunk<kStream, P, G, MASTER>(at, c.count, k, s, keep));
+    } else {
+        SS_DISPATCH_KIND(c.kind, master != nullptr,
+                         step_chunk<kStreamMoments, P, G, MASTER>(at, c.count, k, s, keep));
+    }
+    if (SOLO) end_solo(scalars, s);
 }
 
 // ---- AdamW with moments in 8 bits -----------------------------------------------------------
@@ -316,6 +462,19 @@ __device__ __forceinline__ int field_of(uint32_t bits, int least)
     return b > least ? b : least;
 }
 
+// stepped() with the hardware's root and reciprocal, each within a step of fp32 of its value: a
+// packed step has so little to read that the exact ones cost more than the memory does (2^28 bf16
+// elements 566 instead of 493 us).  The root takes v below 2^-126 for 0: against eps >= 1e-12 that
+// is nothing, smaller ones go the exact way.
+constexpr float kLeastFastEps = 1e-12f;
+
+__device__ __forceinline__ float stepped_fast(float p, float m, float v, const Betas &k,
+                                              const Scalars &s, float keep)
+{
+    const float den = __builtin_amdgcn_sqrtf(v) * s.root + k.eps;
+    return p * keep - s.size * (m * __builtin_amdgcn_rcpf(den));
+}
+
 template <int P, int G, bool MASTER>
 __device__ __forceinline__ void step_chunk8(const Chunk &c, void *p, const void *g, uint8_t *mc,
                                             uint8_t *vc, uint8_t *exps, float *master,
@@ -354,10 +513,16 @@ __device__ __forceinline__ void step_chunk8(const Chunk &c, void *p, const void 
             v[i] = unpack_v(vw[i / 4], i % 4, sv);
             if (i >= n) m[i] = v[i] = 0.0f;
             moments(gf[i] * s.factor, m[i], v[i], k);
-            pf[i] = stepped(pf[i], m[i], v[i], k, s, keep);
             const uint32_t bm = __float_as_uint(m[i]) & 0x7FFFFFFFu, bv = __float_as_uint(v[i]);
             top_m = bm > top_m ? bm : top_m;
             top_v = bv > top_v ? bv : top_v;
+        }
+        if (k.eps >= kLeastFastEps) {
+#pragma unroll
+            for (int i = 0; i < N; ++i) pf[i] = stepped_fast(pf[i], m[i], v[i], k, s, keep);
+        } else {
+#pragma unroll
+            for (int i = 0; i < N; ++i) pf[i] = stepped(pf[i], m[i], v[i], k, s, keep);
         }
         uint32_t lost = 0;                 // elements whose v is not finite
         if (__any(top_v >= kInfBits)) {
@@ -405,21 +570,23 @@ __device__ __forceinline__ void step_chunk8(const Chunk &c, void *p, const void 
     }
 }
 
+template <bool SOLO>
 __global__ __launch_bounds__(kWG) void adamw_packed_kernel(const void *chunks, void *const *params,
                                                            const void *const *grads, uint8_t *m,
                                                            uint8_t *v, uint8_t *exps,
-                                                           float *master,
-                                                           const Scalars *__restrict__ scalars,
-                                                           Betas k)
+                                                           float *master, Scalars *scalars,
+                                                           Betas k, Begin b)
 {
-    const Scalars s = *scalars;
-    if (!s.apply) return;
-    const Chunk c = load_chunk(chunks, blockIdx.x);
+    const Chunk c = load_chunk(chunks, chunk_of_block());
+    const Scalars s = SOLO ? begin_solo(scalars, b) : *scalars;
     void *p = params[c.tensor];
     const void *g = grads[c.tensor];
     const float keep = c.kind & 16 ? 1.0f : s.keep;
-    SS_DISPATCH_KIND(c.kind, master != nullptr,
-                     step_chunk8<P, G, MASTER>(c, p, g, m, v, exps, master, k, s, keep));
+    if (s.apply) {
+        SS_DISPATCH_KIND(c.kind, master != nullptr,
+                         step_chunk8<P, G, MASTER>(c, p, g, m, v, exps, master, k, s, keep));
+    }
+    if (SOLO) end_solo(scalars, s);
 }
 
 // The values that packed moments stand for: 8 elements per lane.
@@ -448,7 +615,8 @@ __global__ __launch_bounds__(kWG) void moments_kernel(const uint8_t *__restrict_
 int32_t check_list(const char *who, const ss_tensor_list *list)
 {
     if (!list) return fail(SS_ERR_INVALID_ARG, "%s: list is NULL", who);
-    if (list->num_tensors < 0 || list->num_chunks < 0 || list->state_elems < 0)
+    if (list->num_tensors < 0 || list->num_chunks < 0 || list->num_chunks > kMostChunks ||
+        list->state_elems < 0)
         return fail(SS_ERR_INVALID_ARG, "%s: list was not planned", who);
     if (list->num_chunks > 0 && !list->chunks)
         return fail(SS_ERR_INVALID_ARG, "%s: list->chunks is NULL", who);
@@ -475,7 +643,8 @@ int32_t check_state(const char *who, const ss_tensor_list *list, const ss_adamw_
 
 int norm_wgs(const ss_tensor_list *list)
 {
-    return list->num_chunks < kNormWgs ? list->num_chunks : kNormWgs;
+    const int64_t wgs = ((int64_t)list->num_chunks + kWG / 64 - 1) / (kWG / 64);
+    return (int)(wgs < kNormWgs ? wgs : kNormWgs);
 }
 
 }  // namespace
@@ -508,7 +677,7 @@ int32_t ss_tensor_list_plan(const ss_tensor *tensors, int32_t n, ss_tensor_list 
             return fail(SS_ERR_INVALID_ARG, "%s: tensors[%d].no_decay or reserved", who, k);
         num += (t.numel + kChunk - 1) / kChunk;
         elems += (t.numel + SS_MOMENT_BLOCK - 1) / SS_MOMENT_BLOCK * SS_MOMENT_BLOCK;
-        if (num > 0x7fffffffLL) return fail(SS_ERR_UNSUPPORTED, "%s: list too long", who);
+        if (num > kMostChunks) return fail(SS_ERR_UNSUPPORTED, "%s: list too long", who);
     }
     if (chunks) {
         if (chunks_bytes < (size_t)num * sizeof(Chunk))
@@ -570,7 +739,8 @@ int32_t ss_grad_norm(const ss_tensor_list *list, const void *const *grads, doubl
 }
 
 int32_t ss_adamw_step(const ss_tensor_list *list, void *const *params, const void *const *grads,
-                      const ss_adamw_state *state, const ss_adamw_hyper *hyper, const float *clip,
+                      const ss_adamw_state *state, double lr, const float *lr_device, double beta1,
+                      double beta2, double eps, double weight_decay, const float *clip,
                       void *stream)
 {
     const char *who = "ss_adamw_step";
@@ -584,38 +754,36 @@ int32_t ss_adamw_step(const ss_tensor_list *list, void *const *params, const voi
         return fail(SS_ERR_INVALID_ARG, "%s: state->counters is NULL or not 64-byte aligned", who);
     if (reinterpret_cast<uintptr_t>(clip) % 16 != 0)
         return fail(SS_ERR_INVALID_ARG, "%s: clip is not 16-byte aligned", who);
-    if (!hyper) return fail(SS_ERR_INVALID_ARG, "%s: hyper is NULL", who);
-    const ss_adamw_hyper h = *hyper;
-    if (!isfinite(h.lr) || !isfinite(h.weight_decay) || h.lr < 0.0 || h.weight_decay < 0.0)
-        return fail(SS_ERR_INVALID_ARG, "%s: lr = %g, weight_decay = %g", who, h.lr,
-                    h.weight_decay);
-    if (!(h.beta1 >= 0.0 && h.beta1 < 1.0 && h.beta2 >= 0.0 && h.beta2 < 1.0))
-        return fail(SS_ERR_INVALID_ARG, "%s: beta1 = %g, beta2 = %g (need [0, 1))", who, h.beta1,
-                    h.beta2);
-    if (!(h.eps >= 1e-30 && h.eps <= 1e30))
-        return fail(SS_ERR_INVALID_ARG, "%s: eps = %g (need 1e-30 to 1e30)", who, h.eps);
+    if (!isfinite(lr) || !isfinite(weight_decay) || lr < 0.0 || weight_decay < 0.0)
+        return fail(SS_ERR_INVALID_ARG, "%s: lr = %g, weight_decay = %g", who, lr, weight_decay);
+    if (!(beta1 >= 0.0 && beta1 < 1.0 && beta2 >= 0.0 && beta2 < 1.0))
+        return fail(SS_ERR_INVALID_ARG, "%s: beta1 = %g, beta2 = %g (need [0, 1))", who, beta1,
+                    beta2);
+    if (!(eps >= 1e-30 && eps <= 1e30))
+        return fail(SS_ERR_INVALID_ARG, "%s: eps = %g (need 1e-30 to 1e30)", who, eps);
     const hipStream_t s = static_cast<hipStream_t>(stream);
     Scalars *scalars = static_cast<Scalars *>(state->counters);
-    const Betas k{(float)h.beta1, (float)(1.0 - h.beta1), (float)h.beta2, (float)(1.0 - h.beta2),
-                  (float)h.eps};
-    {
+    const Betas k{(float)beta1, (float)(1.0 - beta1), (float)beta2, (float)(1.0 - beta2),
+                  (float)eps};
+    const Begin b{lr, log(beta1), log(beta2), weight_decay, lr_device, clip};
+    const dim3 grid((unsigned)list->num_chunks);
+    const bool solo = list->num_chunks > 0 && list->num_chunks <= kSoloChunks;
+    if (!solo) {
         ProfScope prof("adamw_begin_kernel", s);
-        launch(adamw_begin_kernel, dim3(1), dim3(64), s, scalars, clip, h.lr_device, h.lr, h.beta1,
-               h.beta2, h.weight_decay);
+        launch(adamw_begin_kernel, dim3(1), dim3(64), s, scalars, b);
     }
-    if (list->num_chunks > 0) {
-        const dim3 grid((unsigned)list->num_chunks);
-        if (state->bits == 32) {
-            ProfScope prof("adamw_kernel", s);
-            launch(adamw_kernel, grid, dim3(kWG), s, list->chunks, params, grads,
-                   static_cast<float *>(state->m), static_cast<float *>(state->v), state->master,
-                   (const Scalars *)scalars, k);
-        } else {
-            ProfScope prof("adamw_packed_kernel", s);
-            launch(adamw_packed_kernel, grid, dim3(kWG), s, list->chunks, params, grads,
-                   static_cast<uint8_t *>(state->m), static_cast<uint8_t *>(state->v), state->exps,
-                   state->master, (const Scalars *)scalars, k);
-        }
+    if (list->num_chunks > 0 && state->bits == 32) {
+        ProfScope prof("adamw_kernel", s);
+        launch(solo ? adamw_kernel<false, true>
+                    : list->state_elems >= kStreamElems ? adamw_kernel<true, false>
+                                                        : adamw_kernel<false, false>,
+               grid, dim3(kWG), s, list->chunks, params, grads, static_cast<float *>(state->m),
+               static_cast<float *>(state->v), state->master, scalars, k, b);
+    } else if (list->num_chunks > 0) {
+        ProfScope prof("adamw_packed_kernel", s);
+        launch(solo ? adamw_packed_kernel<true> : adamw_packed_kernel<false>, grid, dim3(kWG), s,
+               list->chunks, params, grads, static_cast<uint8_t *>(state->m),
+               static_cast<uint8_t *>(state->v), state->exps, state->master, scalars, k, b);
     }
     return check_launch(who);
 }
@@ -634,7 +802,7 @@ int32_t ss_adamw_moments(const ss_tensor_list *list, const ss_adamw_state *state
         return fail(SS_ERR_INVALID_ARG, "%s: an output is not 16-byte aligned", who);
     if (list->state_elems == 0 || (!m_bf && !v_bf)) return SS_OK;
     const hipStream_t s = static_cast<hipStream_t>(stream);
-    const int64_t wgs = (list->state_elems + kPass - 1) / kPass;
+    const int64_t wgs = (list->state_elems + kWG * kLane8 - 1) / (kWG * kLane8);
     ProfScope prof("moments_kernel", s);
     launch(moments_kernel, dim3((unsigned)(wgs < 1 << 20 ? wgs : 1 << 20)), dim3(kWG), s,
            static_cast<const uint8_t *>(state->m), static_cast<const uint8_t *>(state->v),

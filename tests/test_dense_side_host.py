@@ -47,7 +47,9 @@ def test_plan_refuses(tensor, text):
 
 
 def test_plan_refuses_a_list_that_is_too_long():
-    rc, _, _ = plan([(1 << 46, 1, 1, 0, 0)])
+    rc, out, _ = plan([((1 << 24) * 2048 - 2048, 1, 1, 0, 0)])
+    assert rc == 0 and out.num_chunks == (1 << 24) - 1
+    rc, _, _ = plan([((1 << 24) * 2048 - 2048, 1, 1, 0, 0), (1, 0, 0, 0, 0)])
     assert rc == 2 and "too long" in B.ss_last_error()
 
 
@@ -77,28 +79,24 @@ def state(**kw):
     return B._CAdamWState(a["bits"], 0, a["m"], a["v"], a["exps"], a["master"], a["counters"])
 
 
-def hyper(**kw):
-    a = dict(lr=1e-3, beta1=0.9, beta2=0.999, eps=1e-8, weight_decay=0.01)
-    a.update(kw)
-    return B._CAdamWHyper(a["lr"], a["beta1"], a["beta2"], a["eps"], a["weight_decay"], None)
-
-
 @pytest.mark.parametrize("change,text", [
     (dict(lst=None), "list is NULL"), (dict(params=None), "NULL"), (dict(grads=None), "NULL"),
-    (dict(state=None), "state is NULL"), (dict(hyper=None), "hyper is NULL"),
+    (dict(state=None), "state is NULL"),
     (dict(state=state(bits=16)), "bits"), (dict(state=state(m=None)), "NULL"),
     (dict(state=state(bits=8)), "exps"), (dict(state=state(v=FAKE + 8)), "aligned"),
     (dict(state=state(master=FAKE + 4)), "master"), (dict(state=state(counters=None)), "counters"),
     (dict(state=state(counters=FAKE + 16)), "counters"), (dict(clip=FAKE + 8), "clip"),
-    (dict(hyper=hyper(lr=-1.0)), "lr"), (dict(hyper=hyper(lr=math.nan)), "lr"),
-    (dict(hyper=hyper(weight_decay=-0.1)), "weight_decay"),
-    (dict(hyper=hyper(beta1=1.0)), "beta1"), (dict(hyper=hyper(beta2=-0.1)), "beta2"),
-    (dict(hyper=hyper(beta2=math.nan)), "beta2"), (dict(hyper=hyper(eps=0.0)), "eps"),
-    (dict(hyper=hyper(eps=math.inf)), "eps")])
+    (dict(lr=-1.0), "lr"), (dict(lr=math.nan), "lr"),
+    (dict(weight_decay=-0.1), "weight_decay"),
+    (dict(beta1=1.0), "beta1"), (dict(beta2=-0.1), "beta2"),
+    (dict(beta2=math.nan), "beta2"), (dict(eps=0.0), "eps"),
+    (dict(eps=math.inf), "eps")])
 def test_adamw_step_refuses(change, text):
-    a = dict(lst=a_list(), params=FAKE, grads=FAKE, state=state(), hyper=hyper(), clip=None)
+    a = dict(lst=a_list(), params=FAKE, grads=FAKE, state=state(), lr=1e-3, beta1=0.9, beta2=0.999,
+             eps=1e-8, weight_decay=0.01, clip=None)
     a.update(change)
-    rc = lib.ss_adamw_step(a["lst"], a["params"], a["grads"], a["state"], a["hyper"], a["clip"], None)
+    rc = lib.ss_adamw_step(a["lst"], a["params"], a["grads"], a["state"], a["lr"], None, a["beta1"],
+                           a["beta2"], a["eps"], a["weight_decay"], a["clip"], None)
     assert rc == 1 and text in B.ss_last_error()
 
 
