@@ -17,37 +17,361 @@ namespace {
 // Elements per 16-byte access.
 template <int DT> constexpr int per_access() { return DT == SS_F32 ? 4 : 8; }
 
-template <int LANES> constexpr int wg_size() { return LANES > kWG ? LANES : kWG; }
+// Threads of a workgroup: forward few, so that several share a compute unit; backward many, since
+// every workgroup ends in a partial row of the parameters' gradients.
+template <int LANES> constexpr int fwd_threads() { return LANES > kWG ? LANES : kWG; }
+template <int LANES> constexpr int bwd_threads() { return LANES > 512 ? LANES : 512; }
 
-// Sum over the group of lanes that owns a row; in all of them.  Groups of several wavefronts are
-// the whole workgroup; `s` then has a float per wavefront and is not used by the sum before.
-template <int LANES>
-__device__ __forceinline__ float row_sum(float v, float *s)
+template <int CTRL> __device__ __forceinline__ float dpp(float v)
 {
-    constexpr int W = LANES < 64 ? LANES : 64;
-#pragma unroll
-    for (int off = W / 2; off > 0; off >>= 1) v += __shfl_xor(v, off, W);
-    if constexpr (LANES > 64) {
-        if (threadIdx.x % 64 == 0) s[threadIdx.x / 64] = v;
-        __syncthreads();
-        v = 0.0f;
-#pragma unroll
-        for (int w = 0; w < LANES / 64; ++w) v += s[w];
+    return __int_as_float(__builtin_amdgcn_update_dpp(0, __float_as_int(v), CTRL, 0xf, 0xf, true));
+}
+// Sum over W lanes (a power of two, at most a wavefront) that start at a multiple of W; in all of
+// them.  Exchanges inside a row of 16 lanes are part of the addition, the two beyond are swaps of rows
+// and of halves: nothing goes through LDS.
+template <int W> __device__ __forceinline__ float lane_sum(float v)
+{
+    if constexpr (W >= 2) v += dpp<0xB1>(v);           // quad_perm 1 0 3 2
+    if constexpr (W >= 4) v += dpp<0x4E>(v);           // quad_perm 2 3 0 1
+    if constexpr (W >= 8) v += dpp<0x141>(v);          // row_half_mirror
+    if constexpr (W >= 16) v += dpp<0x140>(v);         // row_mirror
+    if constexpr (W >= 32) {
+        const auto p = __builtin_amdgcn_permlane16_swap(__float_as_uint(v), __float_as_uint(v), false,
+                                                        false);
+        v = __uint_as_float(p[0]) + __uint_as_float(p[1]);
+    }
+    if constexpr (W >= 64) {
+        const auto p = __builtin_amdgcn_permlane32_swap(__float_as_uint(v), __float_as_uint(v), false,
+                                                        false);
+        v = __uint_as_float(p[0]) + __uint_as_float(p[1]);
     }
     return v;
 }
 
-// A lane's share of a row: P vectors of N elements, LANES vectors apart; zeros past the row.
-template <int DT, int LANES, int P, int N>
-__device__ __forceinline__ void load_share(const void *base, int64_t row, int c, int dim,
-                                           Raw<DT, N> (&r)[P])
+// Sums of K values over the group of lanes that owns a row; in all of them.  A group of several
+// wavefronts passes through `s` (a float per wavefront of the workgroup and value), which is free
+// again behind the next barrier.
+template <int LANES, int K>
+__device__ __forceinline__ void row_sums(float (&v)[K], float *s)
 {
 #pragma unroll
-    for (int i = 0; i < P; ++i) {
-        const int col = (i * LANES + c) * N;
-        if (col + N <= dim) r[i] = load_raw<DT, N>(base, row + col);
-        else r[i] = load_raw_part<DT, N>(base, row + col, dim - col);
+    for (int k = 0; k < K; ++k) v[k] = lane_sum<(LANES < 64 ? LANES : 64)>(v[k]);
+    if constexpr (LANES > 64) {
+        constexpr int WAVES = LANES / 64;
+        const int wave = threadIdx.x / 64;
+        if (threadIdx.x % 64 == 0)
+#pragma unroll
+            for (int k = 0; k < K; ++k) s[wave * K + k] = v[k];
+        __syncthreads();
+        const float *mine = s + wave / WAVES * WAVES * K;
+#pragma unroll
+        for (int k = 0; k < K; ++k) {
+            v[k] = 0.0f;
+#pragma unroll
+            for (int w = 0; w < WAVES; ++w) v[k] += mine[w * K + k];
+        }
     }
+}
+template <int LANES> __device__ __forceinline__ float row_sum(float v, float *s)
+{
+    float one[1] = {v};
+    row_sums<LANES, 1>(one, s);
+    return one[0];
+}
+
+// Columns [col, col + count) of a row belong to a lane's vector of N (count <= 0: none).
+template <int LANES, int N> struct Columns {
+    int col, count;
+    __device__ __forceinline__ Columns(int i, int c, int dim)
+        : col((i * LANES + c) * N), count(dim - col < N ? dim - col : N)
+    {
+    }
+};
+
+// Zeros past the row.  The last vector of a row that is no multiple of N is read where it ends with the
+// row (there is room for that: a row of several lanes is longer than N) and shifted down: one load
+// for a lane where elements taken one by one would cost its whole wavefront N.
+template <int DT, int LANES, int N>
+__device__ __forceinline__ Raw<DT, N> load_columns(const void *base, int64_t row,
+                                                   const Columns<LANES, N> &at)
+{
+    if constexpr (LANES == 1) {
+        if (at.count < N) return load_raw_part<DT, N>(base, row + at.col, at.count);
+        return load_raw<DT, N>(base, row + at.col);
+    } else {
+        typedef uint32_t words __attribute__((ext_vector_type(sizeof(Raw<DT, N>) / 4)));
+        constexpr int W = sizeof(words) / 4, kSize = sizeof(typename Raw<DT, N>::E);
+        Raw<DT, N> r;
+        r.v = 0.0f;
+        if (at.count > 0) {
+            const int skip = N - at.count;
+            r = load_raw<DT, N>(base, row + at.col - skip);
+            if (skip > 0) {
+                words w = __builtin_bit_cast(words, r.v);
+                const int bytes = skip * kSize;
+                if constexpr (W >= 8)
+                    if (bytes & 16)
+#pragma unroll
+                        for (int j = 0; j < W; ++j) w[j] = j + 4 < W ? w[j + 4] : 0u;
+                if (bytes & 8)
+#pragma unroll
+                    for (int j = 0; j < W; ++j) w[j] = j + 2 < W ? w[j + 2] : 0u;
+                if (bytes & 4)
+#pragma unroll
+                    for (int j = 0; j < W; ++j) w[j] = j + 1 < W ? w[j + 1] : 0u;
+                if (kSize == 2 && (bytes & 2))
+#pragma unroll
+                    for (int j = 0; j < W; ++j)
+                        w[j] = __builtin_amdgcn_alignbyte(j + 1 < W ? w[j + 1] : 0u, w[j], 2);
+                r.v = __builtin_bit_cast(typename Raw<DT, N>::V, w);
+            }
+        }
+        return r;
+    }
+}
+template <int DT, int LANES, int N>
+__device__ __forceinline__ void store_columns(void *base, int64_t row, const Columns<LANES, N> &at,
+                                              const float (&f)[N])
+{
+    const Raw<DT, N> r = from_float<DT, N>(f);
+    if (at.count == N) store_raw<DT, N>(base, row + at.col, r);
+    else if (at.count > 0) store_raw_part<DT, N>(base, row + at.col, r, at.count);
+}
+// The parameters of a lane's columns; `absent` where there are none.
+template <int WT, int LANES, int N>
+__device__ __forceinline__ void load_params(const void *p, const Columns<LANES, N> &at, float absent,
+                                            float (&f)[N])
+{
+    if (p) {
+        to_float(load_columns<WT, LANES, N>(p, 0, at), f);
+    } else {
+#pragma unroll
+        for (int k = 0; k < N; ++k) f[k] = absent;
+    }
+}
+// The same bits, which the compiler takes for others: what was worked out of them is worked out again
+// instead of being kept.
+template <int DT, int N> __device__ __forceinline__ void forget(Raw<DT, N> &r)
+{
+    typedef uint32_t words __attribute__((ext_vector_type(sizeof(r.v) / 4)));
+    words w = __builtin_bit_cast(words, r.v);
+    asm("" : "+v"(w));
+    r.v = __builtin_bit_cast(typename Raw<DT, N>::V, w);
+}
+
+// Which of the workgroup's groups of lanes this is: a scalar where wavefronts are not shared, and
+// with it everything that goes by the row.
+template <int LANES> __device__ __forceinline__ uint32_t group_of_lanes()
+{
+    const int g = threadIdx.x / LANES;
+    return LANES >= 64 ? __builtin_amdgcn_readfirstlane(g) : g;
+}
+
+template <int DT, int WT, int LANES, int P>
+__global__ __launch_bounds__(fwd_threads<LANES>()) void rows_forward_kernel(
+    const void *x, int64_t x_stride, int rows, const int32_t *__restrict__ n_valid,
+    const void *gamma, const void *beta, float eps, void *y, int64_t y_stride,
+    float *__restrict__ mean, float *__restrict__ rstd, int dim)
+{
+    constexpr int N = per_access<DT>(), T = fwd_threads<LANES>(), NG = T / LANES;
+    __shared__ float s[2][LANES > 64 ? T / 64 : 1];
+    const uint32_t n = clamp_valid(n_valid, rows), step = gridDim.x * NG;
+    const int c = threadIdx.x % LANES;
+    const float inv = 1.0f / (float)dim;
+    uint32_t r = blockIdx.x * NG + group_of_lanes<LANES>();
+    int64_t x_at = r * x_stride, y_at = r * y_stride;
+    Raw<DT, N> raw[P];
+    const auto ask = [&] {
+#pragma unroll
+        for (int i = 0; i < P; ++i)
+            raw[i] = load_columns<DT>(x, x_at, Columns<LANES, N>(i, c, dim));
+    };
+    if (r < n) ask();
+    float gam[P][N], bet[P][N];
+#pragma unroll
+    for (int i = 0; i < P; ++i) {
+        load_params<WT>(gamma, Columns<LANES, N>(i, c, dim), 1.0f, gam[i]);
+        load_params<WT>(beta, Columns<LANES, N>(i, c, dim), 0.0f, bet[i]);
+    }
+    for (; r < n; r += step, y_at += step * y_stride) {
+        float v[P][N], sum = 0.0f, q = 0.0f;
+#pragma unroll
+        for (int i = 0; i < P; ++i) to_float(raw[i], v[i]);
+        x_at += step * x_stride;
+        if (r + step < n) ask();           // the next row is under way while this one is worked on
+#pragma unroll
+        for (int i = 0; i < P; ++i)
+#pragma unroll
+            for (int e = 0; e < N; ++e) sum += v[i][e];
+        const float mu = row_sum<LANES>(sum, s[0]) * inv;
+#pragma unroll
+        for (int i = 0; i < P; ++i) {
+            const int count = Columns<LANES, N>(i, c, dim).count;
+#pragma unroll
+            for (int e = 0; e < N; ++e) {
+                v[i][e] = e < count ? v[i][e] - mu : 0.0f;
+                q = fmaf(v[i][e], v[i][e], q);
+            }
+        }
+        const float rs = 1.0f / sqrtf(fmaf(row_sum<LANES>(q, s[1]), inv, eps));
+#pragma unroll
+        for (int i = 0; i < P; ++i) {
+            float o[N];
+#pragma unroll
+            for (int e = 0; e < N; ++e) o[e] = fmaf(v[i][e] * rs, gam[i][e], bet[i][e]);
+            store_columns<DT>(y, y_at, Columns<LANES, N>(i, c, dim), o);
+        }
+        if (c == 0) {
+            mean[r] = mu;
+            rstd[r] = rs;
+        }
+    }
+}
+
+template <bool FIRST, typename A, typename B> __device__ __forceinline__ auto &pick(A &a, B &b)
+{
+    if constexpr (FIRST) return a;
+    else return b;
+}
+
+// part: [2][gridDim.x][dim], the products' sums and the gradients' sums; may be null.
+template <int DT, int WT, int LANES, int P>
+__global__ __launch_bounds__(bwd_threads<LANES>()) void rows_backward_kernel(
+    const void *dy, int64_t dy_stride, const void *x, int64_t x_stride, int rows,
+    const int32_t *__restrict__ n_valid, const void *gamma, const float *__restrict__ mean,
+    const float *__restrict__ rstd, void *dx, int64_t dx_stride, int dim,
+    float *__restrict__ part)
+{
+    constexpr int N = per_access<DT>(), T = bwd_threads<LANES>(), NG = T / LANES;
+    constexpr bool kAhead = T <= 512;      // 1024 threads have 128 registers each: not enough
+    __shared__ float s[2][LANES > 64 ? T / 64 * 2 : 1];
+    __shared__ float s_col[NG > 1 ? T * N : 1];
+    const uint32_t n = clamp_valid(n_valid, rows), step = gridDim.x * NG;
+    const int c = threadIdx.x % LANES;
+    const float inv = 1.0f / (float)dim;
+    uint32_t r = blockIdx.x * NG + group_of_lanes<LANES>();
+    int64_t x_at = r * x_stride, dy_at = r * dy_stride, dx_at = r * dx_stride;
+    Raw<DT, N> xn[P], dn[P];               // the next row's
+    float mu_n = 0.0f, rs_n = 0.0f;
+    const auto ask = [&](uint32_t row) {
+#pragma unroll
+        for (int i = 0; i < P; ++i) {
+            const Columns<LANES, N> at(i, c, dim);
+            xn[i] = load_columns<DT>(x, x_at, at);
+            dn[i] = load_columns<DT>(dy, dy_at, at);
+        }
+        mu_n = mean[row];
+        rs_n = rstd[row];
+    };
+    if (kAhead && r < n) ask(r);
+    float gam[kAhead ? P : 1][N], acc_g[P][N], acc_b[P][N];
+    // gamma of vector i's columns: kept, or read again (from the caches) where registers are short
+    const auto gammas = [&](int i) -> float (&)[N] {
+        if constexpr (kAhead) return gam[i];
+        load_params<WT>(gamma, Columns<LANES, N>(i, c, dim), 1.0f, gam[0]);
+        return gam[0];
+    };
+#pragma unroll
+    for (int i = 0; i < P; ++i) {
+        if constexpr (kAhead) load_params<WT>(gamma, Columns<LANES, N>(i, c, dim), 1.0f, gam[i]);
+#pragma unroll
+        for (int e = 0; e < N; ++e) acc_g[i][e] = acc_b[i][e] = 0.0f;
+    }
+    // groups of several wavefronts meet at barriers: all take the turns that the first one has
+    uint32_t lead = blockIdx.x * NG;
+    for (int turn = 0; (LANES > 64 ? lead : r) < n; turn ^= 1) {
+        const bool here = LANES <= 64 || r < n;
+        if (!kAhead && here) ask(r);
+        Raw<DT, N> x_now[kAhead ? P : 1], d_now[kAhead ? P : 1];
+        float sums[2] = {0.0f, 0.0f};
+        const float mu = mu_n, rs = rs_n;
+        if constexpr (kAhead)
+#pragma unroll
+            for (int i = 0; i < P; ++i) x_now[i] = xn[i], d_now[i] = dn[i];
+        auto &xr = pick<kAhead>(x_now, xn);
+        auto &dr = pick<kAhead>(d_now, dn);
+        lead += step;
+        r += step;
+        x_at += step * x_stride;
+        dy_at += step * dy_stride;
+        if (kAhead && r < n) ask(r);       // the next row is under way while this one is worked on
+        if (here) {
+#pragma unroll
+            for (int i = 0; i < P; ++i) {
+                float xf[N], df[N];
+                to_float(xr[i], xf);
+                to_float(dr[i], df);
+                const auto &gm = gammas(i);
+#pragma unroll
+                for (int e = 0; e < N; ++e) {
+                    xf[e] = (xf[e] - mu) * rs;
+                    acc_g[i][e] = fmaf(df[e], xf[e], acc_g[i][e]);
+                    acc_b[i][e] += df[e];
+                    df[e] *= gm[e];                  // 0 past the row
+                    sums[0] += df[e];
+                    sums[1] = fmaf(df[e], xf[e], sums[1]);
+                }
+                if (!kAhead) __builtin_amdgcn_sched_barrier(0);
+            }
+        }
+        row_sums<LANES, 2>(sums, s[turn]);
+        const float m1 = sums[0] * inv, m2 = sums[1] * inv;
+        if (here) {
+#pragma unroll
+            for (int i = 0; i < P; ++i) {
+                float xf[N], df[N], o[N];
+                forget(xr[i]);
+                forget(dr[i]);
+                to_float(xr[i], xf);
+                to_float(dr[i], df);
+                const auto &gm = gammas(i);
+#pragma unroll
+                for (int e = 0; e < N; ++e)
+                    o[e] = fmaf((mu - xf[e]) * rs, m2, fmaf(df[e], gm[e], -m1)) * rs;
+                store_columns<DT>(dx, dx_at, Columns<LANES, N>(i, c, dim), o);
+                if (!kAhead) __builtin_amdgcn_sched_barrier(0);
+            }
+        }
+        dx_at += step * dx_stride;
+    }
+    if (!part) return;
+#pragma unroll
+    for (int which = 0; which < 2; ++which) {
+        float *out = part + ((int64_t)which * gridDim.x + blockIdx.x) * dim;
+#pragma unroll
+        for (int i = 0; i < P; ++i) {
+            const Columns<LANES, N> at(i, c, dim);
+            float t[N];
+#pragma unroll
+            for (int e = 0; e < N; ++e) t[e] = which ? acc_b[i][e] : acc_g[i][e];
+            if constexpr (NG > 1) {                      // the groups' sums, in their order
+                __syncthreads();
+#pragma unroll
+                for (int e = 0; e < N; ++e) s_col[e * T + threadIdx.x] = t[e];
+                __syncthreads();
+                // column j of this vector belongs to element j % N of lane j / N of each group
+                for (int j = threadIdx.x; j < LANES * N; j += T) {
+                    const int col = i * LANES * N + j;
+                    if (col >= dim) break;
+                    float sum = 0.0f;
+                    for (int o = 0; o < NG; ++o) sum += s_col[j % N * T + o * LANES + j / N];
+                    out[col] = sum;
+                }
+            } else {
+                store_columns<SS_F32>(out, 0, at, t);
+            }
+        }
+    }
+}
+
+// ---- rows wider than a workgroup's registers ------------------------------------------------
+constexpr int kWideThreads = 1024;
+
+template <int DT, int N>
+__device__ __forceinline__ Raw<DT, N> load_some(const void *base, int64_t row, int col, int dim)
+{
+    if (col + N <= dim) return load_raw<DT, N>(base, row + col);
+    return load_raw_part<DT, N>(base, row + col, dim - col);
 }
 template <int DT, int N>
 __device__ __forceinline__ void store_some(void *base, int64_t row, int col, int dim,
@@ -57,153 +381,17 @@ __device__ __forceinline__ void store_some(void *base, int64_t row, int col, int
     if (col + N <= dim) store_raw<DT, N>(base, row + col, r);
     else store_raw_part<DT, N>(base, row + col, r, dim - col);
 }
-// The parameters of a lane's columns; `absent` where there are none.
-template <int WT, int LANES, int P, int N>
-__device__ __forceinline__ void load_params(const void *p, int c, int dim, float absent,
-                                            float (&f)[P][N])
+template <int WT, int N>
+__device__ __forceinline__ void some_params(const void *p, int col, int dim, float absent,
+                                            float (&f)[N])
 {
     if (p) {
-        Raw<WT, N> r[P];
-        load_share<WT, LANES, P, N>(p, 0, c, dim, r);
-#pragma unroll
-        for (int i = 0; i < P; ++i) to_float(r[i], f[i]);
+        to_float(load_some<WT, N>(p, 0, col, dim), f);
     } else {
 #pragma unroll
-        for (int i = 0; i < P; ++i)
-#pragma unroll
-            for (int k = 0; k < N; ++k) f[i][k] = absent;
+        for (int k = 0; k < N; ++k) f[k] = absent;
     }
 }
-
-template <int DT, int WT, int LANES, int P>
-__global__ __launch_bounds__(wg_size<LANES>()) void rows_forward_kernel(
-    const void *x, int64_t x_stride, int rows, const int32_t *__restrict__ n_valid,
-    const void *gamma, const void *beta, float eps, void *y, int64_t y_stride,
-    float *__restrict__ mean, float *__restrict__ rstd, int dim)
-{
-    constexpr int N = per_access<DT>(), NG = wg_size<LANES>() / LANES;
-    __shared__ float s[2][LANES > 64 ? LANES / 64 : 1];
-    const int n = clamp_valid(n_valid, rows);
-    const int g = threadIdx.x / LANES, c = threadIdx.x % LANES;
-    const float inv = 1.0f / (float)dim;
-    float gam[P][N], bet[P][N];
-    load_params<WT, LANES, P, N>(gamma, c, dim, 1.0f, gam);
-    load_params<WT, LANES, P, N>(beta, c, dim, 0.0f, bet);
-    for (int64_t r = (int64_t)blockIdx.x * NG + g; r < n; r += (int64_t)gridDim.x * NG) {
-        Raw<DT, N> raw[P];
-        load_share<DT, LANES, P, N>(x, r * x_stride, c, dim, raw);
-        float v[P][N], sum = 0.0f, q = 0.0f;
-#pragma unroll
-        for (int i = 0; i < P; ++i) {
-            to_float(raw[i], v[i]);
-#pragma unroll
-            for (int k = 0; k < N; ++k) sum += v[i][k];
-        }
-        const float mu = row_sum<LANES>(sum, s[0]) * inv;
-#pragma unroll
-        for (int i = 0; i < P; ++i)
-#pragma unroll
-            for (int k = 0; k < N; ++k) {
-                v[i][k] = (i * LANES + c) * N + k < dim ? v[i][k] - mu : 0.0f;
-                q = fmaf(v[i][k], v[i][k], q);
-            }
-        const float rs = 1.0f / sqrtf(fmaf(row_sum<LANES>(q, s[1]), inv, eps));
-#pragma unroll
-        for (int i = 0; i < P; ++i) {
-            float o[N];
-#pragma unroll
-            for (int k = 0; k < N; ++k) o[k] = fmaf(v[i][k] * rs, gam[i][k], bet[i][k]);
-            store_some<DT, N>(y, r * y_stride, (i * LANES + c) * N, dim, o);
-        }
-        if (c == 0) {
-            mean[r] = mu;
-            rstd[r] = rs;
-        }
-    }
-}
-
-// part: [2][gridDim.x][dim], the products' sums and the gradients' sums; may be null.
-template <int DT, int WT, int LANES, int P>
-__global__ __launch_bounds__(wg_size<LANES>()) void rows_backward_kernel(
-    const void *dy, int64_t dy_stride, const void *x, int64_t x_stride, int rows,
-    const int32_t *__restrict__ n_valid, const void *gamma, const float *__restrict__ mean,
-    const float *__restrict__ rstd, void *dx, int64_t dx_stride, int dim,
-    float *__restrict__ part)
-{
-    constexpr int N = per_access<DT>(), NG = wg_size<LANES>() / LANES;
-    __shared__ float s[4][LANES > 64 ? LANES / 64 : 1];
-    __shared__ float s_col[NG > 1 ? kWG * N : 1];
-    const int n = clamp_valid(n_valid, rows);
-    const int g = threadIdx.x / LANES, c = threadIdx.x % LANES;
-    const float inv = 1.0f / (float)dim;
-    float gam[P][N], acc_g[P][N], acc_b[P][N];
-    load_params<WT, LANES, P, N>(gamma, c, dim, 1.0f, gam);
-#pragma unroll
-    for (int i = 0; i < P; ++i)
-#pragma unroll
-        for (int k = 0; k < N; ++k) acc_g[i][k] = acc_b[i][k] = 0.0f;
-    int turn = 0;
-    for (int64_t r = (int64_t)blockIdx.x * NG + g; r < n; r += (int64_t)gridDim.x * NG, turn ^= 2) {
-        Raw<DT, N> xr[P], dr[P];
-        load_share<DT, LANES, P, N>(x, r * x_stride, c, dim, xr);
-        load_share<DT, LANES, P, N>(dy, r * dy_stride, c, dim, dr);
-        const float mu = mean[r], rs = rstd[r];
-        float s1 = 0.0f, s2 = 0.0f;
-#pragma unroll
-        for (int i = 0; i < P; ++i) {
-            float xf[N], df[N];
-            to_float(xr[i], xf);
-            to_float(dr[i], df);
-#pragma unroll
-            for (int k = 0; k < N; ++k) {
-                const float xh = (xf[k] - mu) * rs, gd = gam[i][k] * df[k];
-                s1 += gd;                                // df is 0 past the row
-                s2 = fmaf(gd, xh, s2);
-                acc_g[i][k] = fmaf(df[k], xh, acc_g[i][k]);
-                acc_b[i][k] += df[k];
-            }
-        }
-        const float m1 = row_sum<LANES>(s1, s[turn]) * inv;
-        const float m2 = row_sum<LANES>(s2, s[turn + 1]) * inv;
-#pragma unroll
-        for (int i = 0; i < P; ++i) {
-            float xf[N], df[N], o[N];
-            to_float(xr[i], xf);
-            to_float(dr[i], df);
-#pragma unroll
-            for (int k = 0; k < N; ++k) {
-                const float xh = (xf[k] - mu) * rs;
-                o[k] = fmaf(-xh, m2, fmaf(gam[i][k], df[k], -m1)) * rs;
-            }
-            store_some<DT, N>(dx, r * dx_stride, (i * LANES + c) * N, dim, o);
-        }
-    }
-    if (!part) return;
-#pragma unroll
-    for (int which = 0; which < 2; ++which) {
-        float *out = part + ((int64_t)which * gridDim.x + blockIdx.x) * dim;
-#pragma unroll
-        for (int i = 0; i < P; ++i) {
-            float t[N];
-#pragma unroll
-            for (int k = 0; k < N; ++k) t[k] = which ? acc_b[i][k] : acc_g[i][k];
-            if constexpr (NG > 1) {                      // the groups' sums, in their order
-                __syncthreads();
-#pragma unroll
-                for (int k = 0; k < N; ++k) s_col[k * kWG + threadIdx.x] = t[k];
-                __syncthreads();
-                if (g != 0) continue;
-                for (int o = 1; o < NG; ++o)
-#pragma unroll
-                    for (int k = 0; k < N; ++k) t[k] += s_col[k * kWG + o * LANES + c];
-            }
-            store_some<SS_F32, N>(out, 0, (i * LANES + c) * N, dim, t);
-        }
-    }
-}
-
-// ---- rows wider than a workgroup's registers ------------------------------------------------
-constexpr int kWideThreads = 1024;
 
 template <int DT, int WT>
 __global__ __launch_bounds__(kWideThreads) void wide_forward_kernel(
@@ -220,7 +408,7 @@ __global__ __launch_bounds__(kWideThreads) void wide_forward_kernel(
         for (int col = threadIdx.x * N; col < dim; col += T * N) {
             Raw<DT, N> raw[1];
             float f[N];
-            load_share<DT, 1, 1, N>(x, r * x_stride + col, 0, dim - col, raw);
+            raw[0] = load_some<DT, N>(x, r * x_stride, col, dim);
             to_float(raw[0], f);
 #pragma unroll
             for (int k = 0; k < N; ++k) sum += f[k];
@@ -229,7 +417,7 @@ __global__ __launch_bounds__(kWideThreads) void wide_forward_kernel(
         for (int col = threadIdx.x * N; col < dim; col += T * N) {
             Raw<DT, N> raw[1];
             float f[N];
-            load_share<DT, 1, 1, N>(x, r * x_stride + col, 0, dim - col, raw);
+            raw[0] = load_some<DT, N>(x, r * x_stride, col, dim);
             to_float(raw[0], f);
 #pragma unroll
             for (int k = 0; k < N; ++k) {
@@ -241,12 +429,9 @@ __global__ __launch_bounds__(kWideThreads) void wide_forward_kernel(
         for (int col = threadIdx.x * N; col < dim; col += T * N) {
             Raw<DT, N> raw[1];
             float f[N], gam[1][N], bet[1][N];
-            load_share<DT, 1, 1, N>(x, r * x_stride + col, 0, dim - col, raw);
-            const auto at = [&](const void *p) -> const void * {
-                return p ? static_cast<const typename ElemOf<WT>::type *>(p) + col : nullptr;
-            };
-            load_params<WT, 1, 1, N>(at(gamma), 0, dim - col, 1.0f, gam);
-            load_params<WT, 1, 1, N>(at(beta), 0, dim - col, 0.0f, bet);
+            raw[0] = load_some<DT, N>(x, r * x_stride, col, dim);
+            some_params<WT, N>(gamma, col, dim, 1.0f, gam[0]);
+            some_params<WT, N>(beta, col, dim, 0.0f, bet[0]);
             to_float(raw[0], f);
 #pragma unroll
             for (int k = 0; k < N; ++k) f[k] = fmaf((f[k] - mu) * rs, gam[0][k], bet[0][k]);
@@ -277,11 +462,9 @@ __global__ __launch_bounds__(kWideThreads) void wide_backward_kernel(
             for (int col = threadIdx.x * N; col < dim; col += T * N) {
                 Raw<DT, N> xr[1], dr[1];
                 float xf[N], df[N], gam[1][N];
-                load_share<DT, 1, 1, N>(x, r * x_stride + col, 0, dim - col, xr);
-                load_share<DT, 1, 1, N>(dy, r * dy_stride + col, 0, dim - col, dr);
-                load_params<WT, 1, 1, N>(
-                    gamma ? static_cast<const typename ElemOf<WT>::type *>(gamma) + col : nullptr, 0,
-                    dim - col, 1.0f, gam);
+                xr[0] = load_some<DT, N>(x, r * x_stride, col, dim);
+                dr[0] = load_some<DT, N>(dy, r * dy_stride, col, dim);
+                some_params<WT, N>(gamma, col, dim, 1.0f, gam[0]);
                 to_float(xr[0], xf);
                 to_float(dr[0], df);
 #pragma unroll
@@ -319,8 +502,8 @@ __global__ __launch_bounds__(kWG) void wide_columns_kernel(
     for (int64_t r = blockIdx.y; r < n; r += gridDim.y) {
         Raw<DT, N> xr[1], dr[1];
         float xf[N], df[N];
-        load_share<DT, 1, 1, N>(x, r * x_stride + col, 0, dim - (int)col, xr);
-        load_share<DT, 1, 1, N>(dy, r * dy_stride + col, 0, dim - (int)col, dr);
+        xr[0] = load_some<DT, N>(x, r * x_stride, (int)col, dim);
+        dr[0] = load_some<DT, N>(dy, r * dy_stride, (int)col, dim);
         const float mu = mean[r], rs = rstd[r];
         to_float(xr[0], xf);
         to_float(dr[0], df);
@@ -336,7 +519,7 @@ __global__ __launch_bounds__(kWG) void wide_columns_kernel(
 
 // out[col] = sum of the column's partial sums: thread (p, col) adds every kParts-th row from p on,
 // then the kParts sums are added in order.
-constexpr int kRedCols = 64, kParts = 16;
+constexpr int kRedCols = 32, kParts = 32;
 
 template <int WT>
 __global__ __launch_bounds__(kRedCols * kParts) void columns_reduce_kernel(
@@ -350,8 +533,16 @@ __global__ __launch_bounds__(kRedCols * kParts) void columns_reduce_kernel(
     const float *__restrict__ in = part + (int64_t)blockIdx.y * n_part * dim;
     float sum = 0.0f;
     if (col < dim) {
-#pragma unroll 8
-        for (int w = p; w < n_part; w += kParts) sum += in[(int64_t)w * dim + col];
+        for (int w0 = p; w0 < n_part; w0 += kParts * 8) {
+            float v[8];
+#pragma unroll
+            for (int k = 0; k < 8; ++k) {
+                const int w = w0 + k * kParts;
+                v[k] = w < n_part ? in[(int64_t)w * dim + col] : 0.0f;
+            }
+#pragma unroll
+            for (int k = 0; k < 8; ++k) sum += v[k];
+        }
     }
     s[p][c] = sum;
     __syncthreads();
@@ -368,18 +559,14 @@ struct Shape {
     int lanes, vectors;        // lanes == 0: too wide for registers
 };
 
-Shape shape_of(int dim, int per, int most_vectors)
+Shape shape_of(int dim, int per)
 {
-    const int64_t v = ((int64_t)dim + per - 1) / per;
+    const int v = (dim + per - 1) / per, most = 16 / per;       // vectors of a row; a lane's at most
     int lanes = 1;
     while (lanes < v && lanes < 64) lanes *= 2;
-    if (v <= 64) return {lanes, 1};
-    if (v <= 64 * 2) return {64, 2};
-    if (v <= 64 * 4) return {64, 4};
-    if (v <= 256 * 2) return {256, 2};
-    if (v <= 256 * 4) return {256, 4};
-    if (v <= 1024 * 2) return {1024, 2};
-    if (v <= 1024 * 4 && most_vectors >= 4) return {1024, 4};
+    for (; lanes <= 1024; lanes *= lanes == 64 ? 4 : 2)
+        for (int p = 1; p <= most; p *= 2)
+            if (v <= lanes * p && (lanes <= 256 || p == most)) return {lanes, p};
     return {0, 0};
 }
 
@@ -397,8 +584,12 @@ Shape shape_of(int dim, int per, int most_vectors)
     else SS_ROWS_CASE(4, 1, __VA_ARGS__) else SS_ROWS_CASE(8, 1, __VA_ARGS__)                 \
     else SS_ROWS_CASE(16, 1, __VA_ARGS__) else SS_ROWS_CASE(32, 1, __VA_ARGS__)               \
     else SS_ROWS_CASE(64, 1, __VA_ARGS__) else SS_ROWS_CASE(64, 2, __VA_ARGS__)               \
-    else SS_ROWS_CASE(64, 4, __VA_ARGS__) else SS_ROWS_CASE(256, 2, __VA_ARGS__)              \
-    else SS_ROWS_CASE(256, 4, __VA_ARGS__) else SS_ROWS_CASE(1024, 2, __VA_ARGS__)
+    else SS_ROWS_FULL(64, __VA_ARGS__) else SS_ROWS_CASE(256, 1, __VA_ARGS__)                 \
+    else SS_ROWS_CASE(256, 2, __VA_ARGS__) else SS_ROWS_FULL(256, __VA_ARGS__)                \
+    else SS_ROWS_FULL(512, __VA_ARGS__) else SS_ROWS_FULL(1024, __VA_ARGS__)
+// 16 elements a lane
+#define SS_ROWS_FULL(l, ...)                                                                  \
+    if (sh.lanes == l && sh.vectors == 16 / per_access<DT>()) { constexpr int LANES = l, P = 16 / per_access<DT>(); __VA_ARGS__; }
 
 // Partial rows that the column sums are split into: a workgroup each.  At most kMostParts, and
 // kPartFloats in all (but kLeastParts where a row is that wide).
@@ -423,7 +614,9 @@ int64_t part_floats(int rows, int dim)
     return n < all ? n : all;
 }
 
-constexpr int kForwardWgs = 2048;
+constexpr int kForwardThreads = 256 * 1024;
+constexpr int kWideWgs = 1024;
+constexpr int kBackwardWgs = 256;
 
 int32_t check_rows(const char *who, int32_t dtype, int32_t param_dtype, int32_t rows, int32_t dim)
 {
@@ -476,16 +669,18 @@ int32_t ss_layernorm_rows_forward(int32_t dtype, int32_t param_dtype, int32_t ro
         return fail(SS_ERR_INVALID_ARG, "%s: y is x with another stride", who);
     if (rows == 0) return SS_OK;
     const hipStream_t st = static_cast<hipStream_t>(stream);
-    const Shape sh = shape_of(dim, dtype == SS_F32 ? 4 : 8, 4);
+    const Shape sh = shape_of(dim, dtype == SS_F32 ? 4 : 8);
     ProfScope prof("rows_forward_kernel", st);
 #define SS_ROWS_FWD                                                                           \
-    const int64_t groups = wg_size<LANES>() / LANES, need = (rows + groups - 1) / groups;     \
-    launch(rows_forward_kernel<DT, WT, LANES, P>,                                             \
-           dim3((unsigned)(need < kForwardWgs ? need : kForwardWgs)), dim3(wg_size<LANES>()), \
-           st, x, x_stride, rows, n_valid, gamma, beta, eps, y, y_stride, mean, rstd, dim)
+    const int threads = fwd_threads<LANES>();                                                 \
+    const int64_t groups = threads / LANES, need = (rows + groups - 1) / groups;              \
+    const int64_t most = kForwardThreads / threads;                                           \
+    launch(rows_forward_kernel<DT, WT, LANES, P>, dim3((unsigned)(need < most ? need : most)),\
+           dim3(threads), st, x, x_stride, rows, n_valid, gamma, beta, eps, y, y_stride, mean,\
+           rstd, dim)
     SS_ROWS_TYPES(dtype, param_dtype,
-                  SS_ROWS_SHAPES(SS_ROWS_FWD) else SS_ROWS_CASE(1024, 4, SS_ROWS_FWD) else launch(
-                      wide_forward_kernel<DT, WT>, dim3(rows < kForwardWgs ? rows : kForwardWgs),
+                  SS_ROWS_SHAPES(SS_ROWS_FWD) else launch(
+                      wide_forward_kernel<DT, WT>, dim3(rows < kWideWgs ? rows : kWideWgs),
                       dim3(kWideThreads), st, x, x_stride, rows, n_valid, gamma, beta, eps, y,
                       y_stride, mean, rstd, dim))
 #undef SS_ROWS_FWD
@@ -525,17 +720,20 @@ int32_t ss_layernorm_rows_backward(int32_t dtype, int32_t param_dtype, int32_t r
                     ss_layernorm_rows_workspace_bytes(rows, dim));
     const hipStream_t st = static_cast<hipStream_t>(stream);
     const int per = dtype == SS_F32 ? 4 : 8;
-    const Shape sh = shape_of(dim, per, 2);
+    const Shape sh = shape_of(dim, per);
     float *part = params ? static_cast<float *>(ws) : nullptr;
     int n_part = 0;
     if (rows > 0) {
         const int most = most_parts(rows, dim);
 #define SS_ROWS_BWD                                                                           \
-    const int64_t groups = wg_size<LANES>() / LANES, need = (rows + groups - 1) / groups;     \
+    const int threads = bwd_threads<LANES>();                                                 \
+    const int64_t groups = threads / LANES, need = (rows + groups - 1) / groups;              \
     n_part = (int)(need < most ? need : most);                                                \
+    const int wgs = P > 1 && LANES < 1024 ? kBackwardWgs : 2 * kBackwardWgs;                  \
+    n_part = n_part < wgs ? n_part : wgs;                                                     \
     ProfScope prof("rows_backward_kernel", st);                                               \
-    launch(rows_backward_kernel<DT, WT, LANES, P>, dim3(n_part), dim3(wg_size<LANES>()), st,  \
-           dy, dy_stride, x, x_stride, rows, n_valid, gamma, mean, rstd, dx, dx_stride, dim,  \
+    launch(rows_backward_kernel<DT, WT, LANES, P>, dim3(n_part), dim3(threads), st, dy,       \
+           dy_stride, x, x_stride, rows, n_valid, gamma, mean, rstd, dx, dx_stride, dim,      \
            part)
 #define SS_ROWS_WIDE                                                                          \
     if (params) {                    /* first: dx may be dy or x */                           \
@@ -546,7 +744,7 @@ int32_t ss_layernorm_rows_backward(int32_t dtype, int32_t param_dtype, int32_t r
                part);                                                                         \
     }                                                                                         \
     ProfScope prof("rows_backward_kernel", st);                                               \
-    launch(wide_backward_kernel<DT, WT>, dim3(rows < kForwardWgs ? rows : kForwardWgs),       \
+    launch(wide_backward_kernel<DT, WT>, dim3(rows < kWideWgs ? rows : kWideWgs),             \
            dim3(kWideThreads), st, dy, dy_stride, x, x_stride, rows, n_valid, gamma, mean,    \
            rstd, dx, dx_stride, dim)
         SS_ROWS_TYPES(dtype, param_dtype, SS_ROWS_SHAPES(SS_ROWS_BWD) else { SS_ROWS_WIDE; })
