@@ -569,7 +569,8 @@ int32_t ss_adamw_moments(const ss_tensor_list *list, const ss_adamw_state *state
  *   y may be x itself (same stride), dx may be dy or x.
  * dgamma / dbeta (device [dim], NULL: not wanted): sums over the valid rows in a fixed order, 0
  * where there is none.  If one is given, ws holds ss_layernorm_rows_workspace_bytes(rows, dim)
- * bytes, 256-byte aligned (the size falls in neither argument).
+ * bytes, 256-byte aligned (the size falls in neither argument: a workspace for the largest call serves
+ * the smaller ones; two calls whose work may overlap need one each).
  */
 int32_t ss_layernorm_rows_forward(int32_t dtype, int32_t param_dtype, int32_t rows, int32_t dim,
                                   const void *x, int64_t x_stride, const int32_t *n_valid,

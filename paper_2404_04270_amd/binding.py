@@ -793,7 +793,7 @@ class TensorList:
 
     grads: the gradients, each of its parameter's shape and of its type or fp32; grad_dtypes alone
     leaves them to set_grads.  With neither, the tensors are taken for gradients themselves (a
-    list for ss_grad_norm).  no_decay: truth values, one per tensor.
+    list for ss_grad_norm only).  no_decay: truth values, one per tensor.
     The work table and a first pointer array are copied here, with the host waiting."""
 
     def __init__(self, params: Sequence[torch.Tensor],
@@ -811,8 +811,14 @@ class TensorList:
             _dev_ptr(p, p.dtype, "params")
             if p.device != self.device:
                 raise SlipstreamError("TensorList: the tensors are on several devices")
-        if grads is None and grad_dtypes is None:
+        self.only_grads = grads is None and grad_dtypes is None
+        if self.only_grads:
             grads = self.params
+        else:                                    # a step writes them: each element belongs to one
+            spans = sorted((p.data_ptr(), p.data_ptr() + p.numel() * p.element_size())
+                           for p in self.params if p.numel())
+            if any(a[1] > b[0] for a, b in zip(spans, spans[1:])):
+                raise SlipstreamError("TensorList: two parameters overlap, or one is there twice")
         if grad_dtypes is None:
             grad_dtypes = [g.dtype for g in grads]
         self.grad_dtypes = list(grad_dtypes)
@@ -861,7 +867,7 @@ class TensorList:
         _here(self.device, "set_grads")
         ptrs = self._check_grads(grads)
         if self._gptr is None:
-            self._gptr = torch.zeros(len(ptrs), dtype=torch.int64, device=self.device)
+            self._gptr = torch.empty(len(ptrs), dtype=torch.int64, device=self.device)
         ss_pointer_table(self._gptr, ptrs, stream)
         self.grads = list(grads)
 
@@ -896,11 +902,14 @@ class AdamWState:
     """Moments of a list's tensors in 32 or in 8 bits, fp32 copies of its 16-bit parameters if
     asked for, and the step's counters: zeros before the first step, made on the current stream.
     Arrays hold the tensors one after the other, each padded to MOMENT_BLOCK elements
-    (TensorList.of cuts one out)."""
+    (TensorList.of cuts one out); a checkpoint holds m, v, exps, master and counters as they are.  A
+    program that writes to 16-bit parameters between steps writes to their copies, too."""
 
     def __init__(self, tensors: TensorList, bits: int = 32, master: bool = False):
         if bits not in (32, 8):
             raise SlipstreamError("AdamWState: moments are held in 32 or in 8 bits")
+        if tensors.only_grads:
+            raise SlipstreamError("AdamWState: the list holds gradients, no parameters")
         n, dev = tensors.state_elems, tensors.device
         dt = torch.float32 if bits == 32 else torch.uint8
         self.bits = bits
@@ -925,9 +934,10 @@ def ss_adamw_step(tensors: TensorList, state: AdamWState, lr, beta1: float = 0.9
                   clip: Optional[torch.Tensor] = None, stream=None) -> None:
     """lr: a number, or a device tensor of one float that is read when the step runs."""
     _here(tensors.device, "ss_adamw_step")
-    if tensors._gptr is None:
-        raise SlipstreamError("ss_adamw_step: the list has no gradients yet (set_grads)")
-    if state.m.numel() != tensors.state_elems:
+    if tensors._gptr is None or tensors.only_grads:
+        raise SlipstreamError("ss_adamw_step: the list has no gradients yet (set_grads), or holds "
+                              "nothing else")
+    if state.m.numel() != tensors.state_elems or state.m.device != tensors.device:
         raise SlipstreamError("ss_adamw_step: the state belongs to another list")
     if clip is not None and clip.numel() < 4:
         raise SlipstreamError("ss_adamw_step: clip needs four floats")

@@ -2,12 +2,19 @@
 // dense vectors of section 3.5 (layernorm.hip has the pooled ones).
 //
 // Bound by HBM: the forward pass reads x and writes y, the backward pass reads dy and x and writes
-// dx.  A group of lanes owns a row and keeps it in registers, so that every element is read once;
-// the statistics come from the registers in two passes (the mean, then the centred squares).
-// Groups are as narrow as the row allows, from one lane to the 1024 of a workgroup; wider rows
-// are read again for each pass, from the caches.  The backward pass gives each workgroup
-// rows a grid apart and sums their products column by column in registers; one partial row per
+// dx.  A group of lanes owns a row and keeps it in registers, so that every element is read once; the
+// statistics come from the registers in two passes (the mean, then the centred squares: a row whose
+// mean is large against its spread keeps its digits).  Groups are as narrow as the row allows, from
+// one lane to a workgroup of 512; wider rows are read again for each pass, from the caches.  While a
+// group works on a row its next one is being loaded.  The backward pass gives a workgroup rows that
+// are a grid apart and sums their products column by column in registers; one partial row per
 // workgroup goes to memory, and a second kernel adds those in order.
+//
+// us, and TB/s of x, y, dy and dx (a device-wide addition of a constant reaches 6.2): forward
+// 16384 x 8192 bf16 95 (5.6), 65536 x 512 fp16 26 (5.2), 10007 x 1001 fp32 13.3 (6.0, partly from the
+// last-level cache); backward 32768 x 4096 bf16 150 (5.4), 16384 x 4096 fp32 155 (5.2),
+// 16384 x 1024 bf16 24.6 (4.1), 10007 x 1001 fp16 17.9 (3.4), each with about 4 us for the second
+// kernel.
 #include "elem_io.h"
 #include "ss_common.h"
 
@@ -17,8 +24,9 @@ namespace {
 // Elements per 16-byte access.
 template <int DT> constexpr int per_access() { return DT == SS_F32 ? 4 : 8; }
 
-// Threads of a workgroup: forward few, so that several share a compute unit; backward many, since
-// every workgroup ends in a partial row of the parameters' gradients.
+// Threads of a workgroup: forward few, so that several share a compute unit; backward more, since
+// every workgroup ends in a partial row of the parameters' gradients.  (With 1024 each of them has
+// 128 registers and spills: 32768 x 4096 bf16 backward 159 us, 150 with 512.)
 template <int LANES> constexpr int fwd_threads() { return LANES > kWG ? LANES : kWG; }
 template <int LANES> constexpr int bwd_threads() { return LANES > 512 ? LANES : 512; }
 
@@ -90,52 +98,76 @@ template <int LANES, int N> struct Columns {
 
 // Zeros past the row.  The last vector of a row that is no multiple of N is read where it ends with the
 // row (there is room for that: a row of several lanes is longer than N) and shifted down: one load
-// for a lane where elements taken one by one would cost its whole wavefront N.
+// for a lane where elements taken one by one would cost its whole wavefront N.  The shift is a step
+// of its own, so that asking for a row does not wait for it.
 template <int DT, int LANES, int N>
-__device__ __forceinline__ Raw<DT, N> load_columns(const void *base, int64_t row,
-                                                   const Columns<LANES, N> &at)
+__device__ __forceinline__ Raw<DT, N> ask_columns(const void *base, int64_t row,
+                                                  const Columns<LANES, N> &at)
 {
     if constexpr (LANES == 1) {
         if (at.count < N) return load_raw_part<DT, N>(base, row + at.col, at.count);
         return load_raw<DT, N>(base, row + at.col);
-    } else {
-        typedef uint32_t words __attribute__((ext_vector_type(sizeof(Raw<DT, N>) / 4)));
-        constexpr int W = sizeof(words) / 4, kSize = sizeof(typename Raw<DT, N>::E);
-        Raw<DT, N> r;
-        r.v = 0.0f;
-        if (at.count > 0) {
-            const int skip = N - at.count;
-            r = load_raw<DT, N>(base, row + at.col - skip);
-            if (skip > 0) {
-                words w = __builtin_bit_cast(words, r.v);
-                const int bytes = skip * kSize;
-                if constexpr (W >= 8)
-                    if (bytes & 16)
-#pragma unroll
-                        for (int j = 0; j < W; ++j) w[j] = j + 4 < W ? w[j + 4] : 0u;
-                if (bytes & 8)
-#pragma unroll
-                    for (int j = 0; j < W; ++j) w[j] = j + 2 < W ? w[j + 2] : 0u;
-                if (bytes & 4)
-#pragma unroll
-                    for (int j = 0; j < W; ++j) w[j] = j + 1 < W ? w[j + 1] : 0u;
-                if (kSize == 2 && (bytes & 2))
-#pragma unroll
-                    for (int j = 0; j < W; ++j)
-                        w[j] = __builtin_amdgcn_alignbyte(j + 1 < W ? w[j + 1] : 0u, w[j], 2);
-                r.v = __builtin_bit_cast(typename Raw<DT, N>::V, w);
-            }
-        }
-        return r;
     }
+    Raw<DT, N> r;
+    r.v = 0.0f;
+    if (at.count > 0) r = load_raw<DT, N>(base, row + at.col + at.count - N);
+    return r;
 }
+template <int DT, int LANES, int N>
+__device__ __forceinline__ void settle(Raw<DT, N> &r, const Columns<LANES, N> &at)
+{
+    if (LANES == 1 || at.count == N || at.count <= 0) return;
+    typedef uint32_t words __attribute__((ext_vector_type(sizeof(Raw<DT, N>) / 4)));
+    constexpr int W = sizeof(words) / 4, kSize = sizeof(typename Raw<DT, N>::E);
+    words w = __builtin_bit_cast(words, r.v);
+    const int bytes = (N - at.count) * kSize;
+    if constexpr (W >= 8)
+        if (bytes & 16)
+#pragma unroll
+            for (int j = 0; j < W; ++j) w[j] = j + 4 < W ? w[j + 4] : 0u;
+    if (bytes & 8)
+#pragma unroll
+        for (int j = 0; j < W; ++j) w[j] = j + 2 < W ? w[j + 2] : 0u;
+    if (bytes & 4)
+#pragma unroll
+        for (int j = 0; j < W; ++j) w[j] = j + 1 < W ? w[j + 1] : 0u;
+    if (kSize == 2 && (bytes & 2))
+#pragma unroll
+        for (int j = 0; j < W; ++j)
+            w[j] = __builtin_amdgcn_alignbyte(j + 1 < W ? w[j + 1] : 0u, w[j], 2);
+    r.v = __builtin_bit_cast(typename Raw<DT, N>::V, w);
+}
+// The first n of four, n < 4.
+template <int DT>
+__device__ __forceinline__ void store_rest(void *base, int64_t at, int n, const Raw<DT, 4> &r)
+{
+    Raw<DT, 2> two;
+    two.v = __builtin_shufflevector(r.v, r.v, 0, 1);
+    if (n & 2) store_raw<DT, 2>(base, at, two);
+    Raw<DT, 1> one;
+    one.v = n & 2 ? r.v[2] : r.v[0];
+    if (n & 1) store_raw<DT, 1>(base, at + (n & 2), one);
+}
+// A row's rest of fewer than N columns: in up to log2(N) stores.
 template <int DT, int LANES, int N>
 __device__ __forceinline__ void store_columns(void *base, int64_t row, const Columns<LANES, N> &at,
                                               const float (&f)[N])
 {
     const Raw<DT, N> r = from_float<DT, N>(f);
-    if (at.count == N) store_raw<DT, N>(base, row + at.col, r);
-    else if (at.count > 0) store_raw_part<DT, N>(base, row + at.col, r, at.count);
+    if (at.count == N) {
+        store_raw<DT, N>(base, row + at.col, r);
+    } else if (at.count > 0) {
+        if constexpr (N == 8) {
+            Raw<DT, 4> four;
+            four.v = __builtin_shufflevector(r.v, r.v, 0, 1, 2, 3);
+            const bool low = (at.count & 4) != 0;
+            if (low) store_raw<DT, 4>(base, row + at.col, four);
+            four.v = low ? __builtin_shufflevector(r.v, r.v, 4, 5, 6, 7) : four.v;
+            store_rest<DT>(base, row + at.col + (at.count & 4), at.count & 3, four);
+        } else {
+            store_rest<DT>(base, row + at.col, at.count, r);
+        }
+    }
 }
 // The parameters of a lane's columns; `absent` where there are none.
 template <int WT, int LANES, int N>
@@ -143,7 +175,9 @@ __device__ __forceinline__ void load_params(const void *p, const Columns<LANES, 
                                             float (&f)[N])
 {
     if (p) {
-        to_float(load_columns<WT, LANES, N>(p, 0, at), f);
+        Raw<WT, N> r = ask_columns<WT>(p, 0, at);
+        settle(r, at);
+        to_float(r, f);
     } else {
 #pragma unroll
         for (int k = 0; k < N; ++k) f[k] = absent;
@@ -184,7 +218,7 @@ __global__ __launch_bounds__(fwd_threads<LANES>()) void rows_forward_kernel(
     const auto ask = [&] {
 #pragma unroll
         for (int i = 0; i < P; ++i)
-            raw[i] = load_columns<DT>(x, x_at, Columns<LANES, N>(i, c, dim));
+            raw[i] = ask_columns<DT>(x, x_at, Columns<LANES, N>(i, c, dim));
     };
     if (r < n) ask();
     float gam[P][N], bet[P][N];
@@ -196,7 +230,10 @@ __global__ __launch_bounds__(fwd_threads<LANES>()) void rows_forward_kernel(
     for (; r < n; r += step, y_at += step * y_stride) {
         float v[P][N], sum = 0.0f, q = 0.0f;
 #pragma unroll
-        for (int i = 0; i < P; ++i) to_float(raw[i], v[i]);
+        for (int i = 0; i < P; ++i) {
+            settle(raw[i], Columns<LANES, N>(i, c, dim));
+            to_float(raw[i], v[i]);
+        }
         x_at += step * x_stride;
         if (r + step < n) ask();           // the next row is under way while this one is worked on
 #pragma unroll
@@ -243,7 +280,8 @@ __global__ __launch_bounds__(bwd_threads<LANES>()) void rows_backward_kernel(
     float *__restrict__ part)
 {
     constexpr int N = per_access<DT>(), T = bwd_threads<LANES>(), NG = T / LANES;
-    constexpr bool kAhead = T <= 512;      // 1024 threads have 128 registers each: not enough
+    // a lane with 32 elements has no registers left for gamma and the next row
+    constexpr bool kKeep = P * N <= 16, kAhead = kKeep;
     __shared__ float s[2][LANES > 64 ? T / 64 * 2 : 1];
     __shared__ float s_col[NG > 1 ? T * N : 1];
     const uint32_t n = clamp_valid(n_valid, rows), step = gridDim.x * NG;
@@ -257,23 +295,23 @@ __global__ __launch_bounds__(bwd_threads<LANES>()) void rows_backward_kernel(
 #pragma unroll
         for (int i = 0; i < P; ++i) {
             const Columns<LANES, N> at(i, c, dim);
-            xn[i] = load_columns<DT>(x, x_at, at);
-            dn[i] = load_columns<DT>(dy, dy_at, at);
+            xn[i] = ask_columns<DT>(x, x_at, at);
+            dn[i] = ask_columns<DT>(dy, dy_at, at);
         }
         mu_n = mean[row];
         rs_n = rstd[row];
     };
     if (kAhead && r < n) ask(r);
-    float gam[kAhead ? P : 1][N], acc_g[P][N], acc_b[P][N];
+    float gam[kKeep ? P : 1][N], acc_g[P][N], acc_b[P][N];
     // gamma of vector i's columns: kept, or read again (from the caches) where registers are short
     const auto gammas = [&](int i) -> float (&)[N] {
-        if constexpr (kAhead) return gam[i];
+        if constexpr (kKeep) return gam[i];
         load_params<WT>(gamma, Columns<LANES, N>(i, c, dim), 1.0f, gam[0]);
         return gam[0];
     };
 #pragma unroll
     for (int i = 0; i < P; ++i) {
-        if constexpr (kAhead) load_params<WT>(gamma, Columns<LANES, N>(i, c, dim), 1.0f, gam[i]);
+        if constexpr (kKeep) load_params<WT>(gamma, Columns<LANES, N>(i, c, dim), 1.0f, gam[i]);
 #pragma unroll
         for (int e = 0; e < N; ++e) acc_g[i][e] = acc_b[i][e] = 0.0f;
     }
@@ -299,6 +337,8 @@ __global__ __launch_bounds__(bwd_threads<LANES>()) void rows_backward_kernel(
 #pragma unroll
             for (int i = 0; i < P; ++i) {
                 float xf[N], df[N];
+                settle(xr[i], Columns<LANES, N>(i, c, dim));
+                settle(dr[i], Columns<LANES, N>(i, c, dim));
                 to_float(xr[i], xf);
                 to_float(dr[i], df);
                 const auto &gm = gammas(i);
@@ -311,7 +351,7 @@ __global__ __launch_bounds__(bwd_threads<LANES>()) void rows_backward_kernel(
                     sums[0] += df[e];
                     sums[1] = fmaf(df[e], xf[e], sums[1]);
                 }
-                if (!kAhead) __builtin_amdgcn_sched_barrier(0);
+                if (!kKeep) __builtin_amdgcn_sched_barrier(0);
             }
         }
         row_sums<LANES, 2>(sums, s[turn]);
@@ -329,7 +369,7 @@ __global__ __launch_bounds__(bwd_threads<LANES>()) void rows_backward_kernel(
                 for (int e = 0; e < N; ++e)
                     o[e] = fmaf((mu - xf[e]) * rs, m2, fmaf(df[e], gm[e], -m1)) * rs;
                 store_columns<DT>(dx, dx_at, Columns<LANES, N>(i, c, dim), o);
-                if (!kAhead) __builtin_amdgcn_sched_barrier(0);
+                if (!kKeep) __builtin_amdgcn_sched_barrier(0);
             }
         }
         dx_at += step * dx_stride;
@@ -553,8 +593,10 @@ __global__ __launch_bounds__(kRedCols * kParts) void columns_reduce_kernel(
 }
 
 // ---- which kernel takes a row ---------------------------------------------------------------
-// Lanes of a row and vectors per lane: the narrowest group whose lanes hold the row in one vector
-// each, up to a wavefront; then two and four vectors per lane, then several wavefronts.
+// The narrowest group whose lanes hold the row in one vector each, up to a wavefront (sums then stay
+// within rows of lanes); then up to 16 elements per lane, of one, four and eight wavefronts, which a
+// barrier joins; then 32 per lane.  (8192 to 16384 elements as 16 per lane of 1024 threads spill:
+// 4096 x 16384 bf16 backward 126 to 149 us, 110 with 512.)
 struct Shape {
     int lanes, vectors;        // lanes == 0: too wide for registers
 };
@@ -564,9 +606,10 @@ Shape shape_of(int dim, int per)
     const int v = (dim + per - 1) / per, most = 16 / per;       // vectors of a row; a lane's at most
     int lanes = 1;
     while (lanes < v && lanes < 64) lanes *= 2;
-    for (; lanes <= 1024; lanes *= lanes == 64 ? 4 : 2)
+    for (; lanes <= 512; lanes *= lanes == 64 ? 4 : 2)
         for (int p = 1; p <= most; p *= 2)
             if (v <= lanes * p && (lanes <= 256 || p == most)) return {lanes, p};
+    if (v <= 512 * 2 * most) return {512, 2 * most};
     return {0, 0};
 }
 
@@ -586,7 +629,9 @@ Shape shape_of(int dim, int per)
     else SS_ROWS_CASE(64, 1, __VA_ARGS__) else SS_ROWS_CASE(64, 2, __VA_ARGS__)               \
     else SS_ROWS_FULL(64, __VA_ARGS__) else SS_ROWS_CASE(256, 1, __VA_ARGS__)                 \
     else SS_ROWS_CASE(256, 2, __VA_ARGS__) else SS_ROWS_FULL(256, __VA_ARGS__)                \
-    else SS_ROWS_FULL(512, __VA_ARGS__) else SS_ROWS_FULL(1024, __VA_ARGS__)
+    else SS_ROWS_FULL(512, __VA_ARGS__) else SS_ROWS_TWICE(__VA_ARGS__)
+#define SS_ROWS_TWICE(...)                                                                    \
+    if (sh.lanes == 512 && sh.vectors == 32 / per_access<DT>()) { constexpr int LANES = 512, P = 32 / per_access<DT>(); __VA_ARGS__; }
 // 16 elements a lane
 #define SS_ROWS_FULL(l, ...)                                                                  \
     if (sh.lanes == l && sh.vectors == 16 / per_access<DT>()) { constexpr int LANES = l, P = 16 / per_access<DT>(); __VA_ARGS__; }
@@ -614,8 +659,14 @@ int64_t part_floats(int rows, int dim)
     return n < all ? n : all;
 }
 
+// Threads of a forward launch: four wavefronts per SIMD.  With half / twice as many 16384 x 2048 bf16
+// takes 34.2 / 26.9 us instead of 26.6, 16384 x 1024 14.5 / 14.5 instead of 13.2.
 constexpr int kForwardThreads = 256 * 1024;
 constexpr int kWideWgs = 1024;
+// Workgroups of a backward launch: one per compute unit.  Two where a lane has one vector of a row,
+// and so half as much under way: 16384 x 2048 bf16 44 us with two and 55 with one, 300000 x 100
+// fp32 71 and 81.  Elsewhere the second adds partial rows and nothing else: 32768 x 4096 bf16 157 and
+// 150, 2048 x 4096 19.6 and 17.2, 16384 x 1024 29.3 and 24.4.
 constexpr int kBackwardWgs = 256;
 
 int32_t check_rows(const char *who, int32_t dtype, int32_t param_dtype, int32_t rows, int32_t dim)
@@ -729,7 +780,7 @@ int32_t ss_layernorm_rows_backward(int32_t dtype, int32_t param_dtype, int32_t r
     const int threads = bwd_threads<LANES>();                                                 \
     const int64_t groups = threads / LANES, need = (rows + groups - 1) / groups;              \
     n_part = (int)(need < most ? need : most);                                                \
-    const int wgs = P > 1 && LANES < 1024 ? kBackwardWgs : 2 * kBackwardWgs;                  \
+    const int wgs = P > 1 ? kBackwardWgs : 2 * kBackwardWgs;                                  \
     n_part = n_part < wgs ? n_part : wgs;                                                     \
     ProfScope prof("rows_backward_kernel", st);                                               \
     launch(rows_backward_kernel<DT, WT, LANES, P>, dim3(n_part), dim3(threads), st, dy,       \

@@ -220,3 +220,56 @@ def test_captured_passes_replay():
         graph.replay()
         torch.cuda.synchronize()
         assert all(torch.equal(a, b) for a, b in zip(eager, cap)), n
+
+
+def test_offsets_beyond_32_bits():
+    """Rows 2^29 + 1 elements apart: the later ones start beyond 2^32 bytes and 2^31 elements."""
+    from paper_2404_04270_amd import binding as B
+    gen = torch.Generator(device=DEV).manual_seed(6)
+    rows, dim, stride = 6, 5000, 2 ** 29 + 1
+    wide = torch.empty(stride * (rows - 1) + dim, dtype=BF16, device=DEV)
+    far = wide.as_strided((rows, dim), (stride, 1))
+    x, dy = torch.randn(2, rows, dim, device=DEV, generator=gen).to(BF16).unbind(0)
+    gamma, beta = torch.randn(2, dim, device=DEV, generator=gen).unbind(0)
+    ws = torch.empty(B.ss_layernorm_rows_workspace_bytes(rows, dim), dtype=torch.uint8, device=DEV)
+
+    def out():
+        return torch.empty_like(x), torch.empty(rows, device=DEV), torch.empty(rows, device=DEV)
+
+    near_y, mean, rstd = out()
+    B.ss_layernorm_rows_forward(x, None, gamma, beta, EPS, near_y, mean, rstd)
+    far.copy_(x)
+    y, mean2, rstd2 = out()
+    B.ss_layernorm_rows_forward(far, None, gamma, beta, EPS, y, mean2, rstd2)
+    assert torch.equal(y, near_y) and torch.equal(mean, mean2) and torch.equal(rstd, rstd2)
+    B.ss_layernorm_rows_forward(far, None, gamma, beta, EPS, far, mean2, rstd2)
+    assert torch.equal(far, near_y)
+    dx, dg, db = torch.empty_like(x), torch.empty_like(gamma), torch.empty_like(gamma)
+    B.ss_layernorm_rows_backward(dy, x, None, gamma, mean, rstd, dx, dg, db, ws)
+    far.copy_(dy)
+    dg2, db2 = torch.empty_like(gamma), torch.empty_like(gamma)
+    B.ss_layernorm_rows_backward(far, x, None, gamma, mean, rstd, far, dg2, db2, ws)
+    assert torch.equal(far, dx) and torch.equal(dg, dg2) and torch.equal(db, db2)
+
+
+def test_refusals_of_the_python_calls():
+    from paper_2404_04270_amd import binding as B
+    x = torch.randn(4, 8, device=DEV)
+    y, mean, rstd = torch.empty_like(x), torch.empty(4, device=DEV), torch.empty(4, device=DEV)
+    g = torch.ones(8, device=DEV)
+
+    def forward(x=x, gamma=g, beta=g, y=y, mean=mean, rstd=rstd, eps=EPS, n_valid=None):
+        B.ss_layernorm_rows_forward(x, n_valid, gamma, beta, eps, y, mean, rstd)
+
+    forward()
+    for bad in (dict(x=x.t()), dict(x=x[None]), dict(x=x.double()), dict(y=y.to(BF16)),
+                dict(y=torch.empty(4, 9, device=DEV)), dict(gamma=g[:7]), dict(gamma=g.to(BF16)),
+                dict(beta=g.double()), dict(gamma=torch.ones(16, device=DEV)[::2]),
+                dict(mean=mean[:3]), dict(rstd=rstd.double()), dict(eps=-1.0),
+                dict(x=x[:1].expand(4, 8)), dict(y=y.cpu()), dict(n_valid=torch.ones(1, device=DEV))):
+        with pytest.raises(B.SlipstreamError):
+            forward(**bad)
+    with pytest.raises(B.SlipstreamError):               # parameters of two types
+        forward(x=x.to(BF16), y=y.to(BF16), gamma=g, beta=g.to(BF16))
+    with pytest.raises(B.SlipstreamError, match="workspace"):
+        B.ss_layernorm_rows_backward(x, x, None, g, mean, rstd, y, g.clone(), None, None)
