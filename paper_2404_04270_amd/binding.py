@@ -787,6 +787,15 @@ def _here(device: torch.device, who: str) -> None:
                               "device")
 
 
+def _ptr_on(t: Optional[torch.Tensor], dtype, name: str, index: int):
+    """_ptr, of a tensor on device `index`."""
+    if t is None:
+        return None
+    if t.get_device() != index:
+        raise SlipstreamError(f"{name}: need a tensor on device {index}, got one on {t.device}")
+    return _ptr(t, dtype, name)
+
+
 class TensorList:
     """The tensors of a model (contiguous, fp32 / bf16 / fp16, views at any place of a buffer among
     them), with the work table and the pointer arrays that ss_grad_norm and ss_adamw_step read.
@@ -894,8 +903,8 @@ def ss_grad_norm(tensors: TensorList, max_norm: float, clip: torch.Tensor, ws: t
         raise SlipstreamError("ss_grad_norm: clip needs four floats")
     _check(_lib.ss_grad_norm(
         tensors.c, tensors._gptr.data_ptr(), max_norm, grad_scale,
-        _ptr(clip, torch.float32, "clip"), _ptr(ws, torch.uint8, "ws"), ws.numel(),
-        _stream_ptr(stream)))
+        _ptr_on(clip, torch.float32, "clip", tensors.device.index),
+        _ptr_on(ws, torch.uint8, "ws", tensors.device.index), ws.numel(), _stream_ptr(stream)))
 
 
 class AdamWState:
@@ -945,10 +954,11 @@ def ss_adamw_step(tensors: TensorList, state: AdamWState, lr, beta1: float = 0.9
     if isinstance(lr, torch.Tensor):
         if lr.numel() != 1:
             raise SlipstreamError("ss_adamw_step: lr needs one float")
-        lr, at = 0.0, _ptr(lr, torch.float32, "lr")
+        lr, at = 0.0, _ptr_on(lr, torch.float32, "lr", tensors.device.index)
     _check(_lib.ss_adamw_step(
         tensors.c, tensors._pptr.data_ptr(), tensors._gptr.data_ptr(), state.c, lr, at, beta1,
-        beta2, eps, weight_decay, _ptr(clip, torch.float32, "clip"), _stream_ptr(stream)))
+        beta2, eps, weight_decay, _ptr_on(clip, torch.float32, "clip", tensors.device.index),
+        _stream_ptr(stream)))
 
 
 def ss_adamw_moments(tensors: TensorList, state: AdamWState, m: Optional[torch.Tensor],
@@ -961,8 +971,8 @@ def ss_adamw_moments(tensors: TensorList, state: AdamWState, m: Optional[torch.T
     if state.m.numel() != tensors.state_elems:
         raise SlipstreamError("ss_adamw_moments: the state belongs to another list")
     _check(_lib.ss_adamw_moments(
-        tensors.c, state.c, _ptr(m, torch.bfloat16, "m"), _ptr(v, torch.bfloat16, "v"),
-        _stream_ptr(stream)))
+        tensors.c, state.c, _ptr_on(m, torch.bfloat16, "m", tensors.device.index),
+        _ptr_on(v, torch.bfloat16, "v", tensors.device.index), _stream_ptr(stream)))
 
 
 def _matrix(who: str, name: str, t: torch.Tensor, like: torch.Tensor, shape):
@@ -1010,12 +1020,13 @@ def ss_layernorm_rows_forward(x: torch.Tensor, n_valid: Optional[torch.Tensor],
     """x, y [rows, dim] (rows may be a stride apart); gamma, beta [dim]; mean, rstd fp32 [rows]."""
     who = "ss_layernorm_rows_forward"
     shape, dt, wt = _rows_args(who, x, (gamma, beta), mean, rstd)
+    on = x.get_device()
     xp, xs = _matrix(who, "x", x, x, shape)
     yp, ys = _matrix(who, "y", y, x, shape)
     _check(_lib.ss_layernorm_rows_forward(
-        dt, DTYPES[wt], shape[0], shape[1], xp, xs, _ptr(n_valid, torch.int32, "n_valid"),
+        dt, DTYPES[wt], shape[0], shape[1], xp, xs, _ptr_on(n_valid, torch.int32, "n_valid", on),
         _ptr(gamma, wt, "gamma"), _ptr(beta, wt, "beta"), eps, yp, ys,
-        _ptr(mean, torch.float32, "mean"), _ptr(rstd, torch.float32, "rstd"),
+        _ptr_on(mean, torch.float32, "mean", on), _ptr_on(rstd, torch.float32, "rstd", on),
         _stream_ptr(stream)))
 
 
@@ -1030,14 +1041,15 @@ def ss_layernorm_rows_backward(dy: torch.Tensor, x: torch.Tensor,
                                ws: Optional[torch.Tensor], stream=None) -> None:
     who = "ss_layernorm_rows_backward"
     shape, dt, wt = _rows_args(who, x, (gamma, dgamma, dbeta), mean, rstd)
+    on = x.get_device()
     dyp, dys = _matrix(who, "dy", dy, x, shape)
     xp, xs = _matrix(who, "x", x, x, shape)
     dxp, dxs = _matrix(who, "dx", dx, x, shape)
     _check(_lib.ss_layernorm_rows_backward(
         dt, DTYPES[wt], shape[0], shape[1], dyp, dys, xp, xs,
-        _ptr(n_valid, torch.int32, "n_valid"), _ptr(gamma, wt, "gamma"),
-        _ptr(mean, torch.float32, "mean"), _ptr(rstd, torch.float32, "rstd"), dxp, dxs,
-        _ptr(dgamma, wt, "dgamma"), _ptr(dbeta, wt, "dbeta"), _ptr(ws, torch.uint8, "ws"),
+        _ptr_on(n_valid, torch.int32, "n_valid", on), _ptr(gamma, wt, "gamma"),
+        _ptr_on(mean, torch.float32, "mean", on), _ptr_on(rstd, torch.float32, "rstd", on), dxp, dxs,
+        _ptr(dgamma, wt, "dgamma"), _ptr(dbeta, wt, "dbeta"), _ptr_on(ws, torch.uint8, "ws", on),
         0 if ws is None else ws.numel(), _stream_ptr(stream)))
 
 

@@ -5,6 +5,11 @@
 // element; with 8-bit moments and 16-bit parameters it is 10.  The work table cuts the tensors into
 // chunks, a workgroup takes a chunk, and every access of a lane is as wide as its elements allow
 // (8 or 16 bytes).  A chunk names its tensor, so that tensors of all sizes and types share a launch.
+//
+// us, and TB/s of what a step cannot do without (a device-wide addition of a constant reaches 6.2):
+// 2^28 fp32 elements 1300 to 1360 (5.5 to 5.8), 2^28 bf16 with master copies 1280 to 1350 (5.6 to
+// 5.9); packed moments: 2^28 bf16 505 (5.3), 2^28 fp32 747 (5.8).  A bf16 step with packed moments
+// is at the end of what its arithmetic allows, too: about 60 instructions per element.
 #include <math.h>
 
 #include "elem_io.h"
@@ -463,10 +468,10 @@ __device__ __forceinline__ int field_of(uint32_t bits, int least)
 }
 
 // stepped() with the hardware's root and reciprocal, each within a step of fp32 of its value: a
-// packed step has so little to read that the exact ones cost more than the memory does (2^28 bf16
-// elements 566 instead of 493 us).  The root takes v below 2^-126 for 0: against eps >= 1e-12 that
+// packed step has so little to read that the exact ones show (2^28 bf16 elements 568 instead of 493
+// us).  The root takes v below 2^-126 for 0: against eps >= 1e-12 that
 // is nothing, smaller ones go the exact way.
-constexpr float kLeastFastEps = 1e-12f;
+constexpr double kLeastFastEps = 1e-12;
 
 __device__ __forceinline__ float stepped_fast(float p, float m, float v, const Betas &k,
                                               const Scalars &s, float keep)
@@ -475,7 +480,14 @@ __device__ __forceinline__ float stepped_fast(float p, float m, float v, const B
     return p * keep - s.size * (m * __builtin_amdgcn_rcpf(den));
 }
 
-template <int P, int G, bool MASTER>
+// Packed moments and master copies go past the caches in lists of any size: 16 M fp32 elements 47 us
+// a step, 51 through the caches, 4 M bf16 elements 12.3 and 12.6, 2^28 fp32 747 and 772.
+template <typename T> __device__ __forceinline__ T past_caches(const void *p)
+{
+    return __builtin_nontemporal_load((gptr<const T>)p);
+}
+
+template <bool EXACT, int P, int G, bool MASTER>
 __device__ __forceinline__ void step_chunk8(const Chunk &c, void *p, const void *g, uint8_t *mc,
                                             uint8_t *vc, uint8_t *exps, float *master,
                                             const Betas &k, const Scalars &s, float keep)
@@ -494,11 +506,11 @@ __device__ __forceinline__ void step_chunk8(const Chunk &c, void *p, const void 
             if (!MASTER) pr = load_raw_part<P, N>(p, at, n);
             gr = load_raw_part<G, N>(g, at, n);
         }
-        const w2 mw = *(gptr<const w2>)(mc + st), vw = *(gptr<const w2>)(vc + st);
+        const w2 mw = past_caches<w2>(mc + st), vw = past_caches<w2>(vc + st);
         const uint32_t ex = *(gptr<const uint16_t>)(exps + st / SS_MOMENT_BLOCK * 2);
         float pf[N], gf[N], m[N], v[N];
         if (MASTER) {
-            const f4 a = *(gptr<const f4>)(master + st), b = *(gptr<const f4>)(master + st + 4);
+            const f4 a = past_caches<f4>(master + st), b = past_caches<f4>(master + st + 4);
 #pragma unroll
             for (int i = 0; i < 4; ++i) pf[i] = a[i], pf[4 + i] = b[i];
         } else {
@@ -517,13 +529,10 @@ __device__ __forceinline__ void step_chunk8(const Chunk &c, void *p, const void 
             top_m = bm > top_m ? bm : top_m;
             top_v = bv > top_v ? bv : top_v;
         }
-        if (k.eps >= kLeastFastEps) {
 #pragma unroll
-            for (int i = 0; i < N; ++i) pf[i] = stepped_fast(pf[i], m[i], v[i], k, s, keep);
-        } else {
-#pragma unroll
-            for (int i = 0; i < N; ++i) pf[i] = stepped(pf[i], m[i], v[i], k, s, keep);
-        }
+        for (int i = 0; i < N; ++i)
+            pf[i] = EXACT ? stepped(pf[i], m[i], v[i], k, s, keep)
+                          : stepped_fast(pf[i], m[i], v[i], k, s, keep);
         uint32_t lost = 0;                 // elements whose v is not finite
         if (__any(top_v >= kInfBits)) {
             top_m = top_v = 0;
@@ -553,15 +562,15 @@ __device__ __forceinline__ void step_chunk8(const Chunk &c, void *p, const void 
             mo[i / 4] |= cm << (8 * (i % 4));
             vo[i / 4] |= cv << (8 * (i % 4));
         }
-        *(gptr<w2>)(mc + st) = mo;
-        *(gptr<w2>)(vc + st) = vo;
+        __builtin_nontemporal_store(mo, (gptr<w2>)(mc + st));
+        __builtin_nontemporal_store(vo, (gptr<w2>)(vc + st));
         if (threadIdx.x % 16 == 0)
             *(gptr<uint16_t>)(exps + st / SS_MOMENT_BLOCK * 2) = (uint16_t)(b_m | b_v << 8);
         if (MASTER) {
 #pragma unroll
             for (int i = 0; i < N; ++i) pf[i] = i < n ? pf[i] : 0.0f;
-            *(gptr<f4>)(master + st) = f4{pf[0], pf[1], pf[2], pf[3]};
-            *(gptr<f4>)(master + st + 4) = f4{pf[4], pf[5], pf[6], pf[7]};
+            __builtin_nontemporal_store(f4{pf[0], pf[1], pf[2], pf[3]}, (gptr<f4>)(master + st));
+            __builtin_nontemporal_store(f4{pf[4], pf[5], pf[6], pf[7]}, (gptr<f4>)(master + st + 4));
         }
         if (MASTER) as_stored(pf);
         const Raw<P, N> pw = from_float<P, N>(pf);
@@ -570,7 +579,7 @@ __device__ __forceinline__ void step_chunk8(const Chunk &c, void *p, const void 
     }
 }
 
-template <bool SOLO>
+template <bool SOLO, bool EXACT>
 __global__ __launch_bounds__(kWG) void adamw_packed_kernel(const void *chunks, void *const *params,
                                                            const void *const *grads, uint8_t *m,
                                                            uint8_t *v, uint8_t *exps,
@@ -584,7 +593,7 @@ __global__ __launch_bounds__(kWG) void adamw_packed_kernel(const void *chunks, v
     const float keep = c.kind & 16 ? 1.0f : s.keep;
     if (s.apply) {
         SS_DISPATCH_KIND(c.kind, master != nullptr,
-                         step_chunk8<P, G, MASTER>(c, p, g, m, v, exps, master, k, s, keep));
+                         step_chunk8<EXACT, P, G, MASTER>(c, p, g, m, v, exps, master, k, s, keep));
     }
     if (SOLO) end_solo(scalars, s);
 }
@@ -781,9 +790,12 @@ int32_t ss_adamw_step(const ss_tensor_list *list, void *const *params, const voi
                static_cast<float *>(state->v), state->master, scalars, k, b);
     } else if (list->num_chunks > 0) {
         ProfScope prof("adamw_packed_kernel", s);
-        launch(solo ? adamw_packed_kernel<true> : adamw_packed_kernel<false>, grid, dim3(kWG), s,
-               list->chunks, params, grads, static_cast<uint8_t *>(state->m),
-               static_cast<uint8_t *>(state->v), state->exps, state->master, scalars, k, b);
+        const bool exact = eps < kLeastFastEps;
+        launch(exact ? solo ? adamw_packed_kernel<true, true> : adamw_packed_kernel<false, true>
+               : solo ? adamw_packed_kernel<true, false> : adamw_packed_kernel<false, false>,
+               grid, dim3(kWG), s, list->chunks, params, grads,
+               static_cast<uint8_t *>(state->m), static_cast<uint8_t *>(state->v), state->exps,
+               state->master, scalars, k, b);
     }
     return check_launch(who);
 }

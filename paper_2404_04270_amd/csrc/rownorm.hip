@@ -587,6 +587,7 @@ __global__ __launch_bounds__(kRedCols * kParts) void columns_reduce_kernel(
     s[p][c] = sum;
     __syncthreads();
     if (p == 0 && col < dim) {
+#pragma unroll
         for (int q = 1; q < kParts; ++q) sum += s[q][c];
         static_cast<typename ElemOf<WT>::type *>(out)[col] = (typename ElemOf<WT>::type)sum;
     }

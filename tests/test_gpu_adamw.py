@@ -379,6 +379,28 @@ def test_another_stream_and_another_clip():
         close(x, want, tol, "clipped")
 
 
+@pytest.mark.parametrize("bits", [32, 8])
+@pytest.mark.parametrize("eps", [1e-30, 9e-13, 1e-12, 1e-3])
+def test_epsilon_on_both_sides_of_the_exact_root(bits, eps):
+    """From 1e-12 on packed steps take the hardware's root and reciprocal, each off by a step of fp32:
+    four half steps more than the 16 counted for the exact ones cover both, so that the bound is
+    taken twice.  Gradients down to 1e-21, whose squares fp32 does not hold: their v is 0 or a few
+    steps of 2^-149, so elements are only looked at where v is a normal number, or m / eps is
+    what is left (eps far above the root)."""
+    from paper_2404_04270_amd import AdamW
+    g0 = torch.logspace(-21, 2, 4000)
+    p, g = torch.zeros(4000, device=DEV), g0.to(DEV)
+    opt = AdamW([p], lr=1.0, eps=eps, weight_decay=0.0, state_bits=bits)
+    opt.set_grads([g])
+    opt.step()
+    want, _, v, tol, _, _ = ref.adamw(torch.zeros(4000), g0, torch.zeros(4000), torch.zeros(4000), 1,
+                                      lr=1.0, eps=eps, weight_decay=0.0)
+    look = v > 1e-37
+    close(p[look.to(DEV)], want[look], 2 * tol[look], eps)
+    if eps >= 1e-12:                     # root below 3.5e-18: less than 4e-6 of eps
+        close(p[~look.to(DEV)], want[~look], 2 * tol[~look] + 4e-6 * want[~look].abs(), eps)
+
+
 def test_same_inputs_give_the_same_bits():
     from paper_2404_04270_amd import AdamW
     outs = []
