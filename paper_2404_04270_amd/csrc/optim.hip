@@ -55,6 +55,9 @@ __device__ __forceinline__ Chunk load_chunk(const void *chunks, int64_t c)
 // and 177.
 constexpr int kNormWgs = 1024;
 constexpr int kFinalThreads = 1024;
+// Up to so many chunks go to one workgroup and one launch: 7.2 instead of 10.1 us from call to call
+// with 1 to 48 chunks, 8.6 and 10.2 with 64 of fp32.
+constexpr int kAloneChunks = 64;
 
 template <int G, int N>
 __device__ __forceinline__ void add_squares(const Raw<G, N> &r, double &sum)
@@ -103,13 +106,14 @@ __device__ __forceinline__ double wg_sum(double v)
 }
 
 // A wavefront takes a chunk at a time; the entry of its next one is fetched meanwhile.
-__global__ __launch_bounds__(kWG) void norm_partial_kernel(const void *chunks, int num_chunks,
-                                                           const void *const *grads,
-                                                           double *__restrict__ part)
+template <int THREADS>
+__device__ __forceinline__ double chunks_squares(const void *chunks, int num_chunks,
+                                                 const void *const *grads)
 {
+    constexpr int kWaves = THREADS / 64;
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64);
-    const int64_t step = (int64_t)gridDim.x * (kWG / 64);
-    int64_t i = (int64_t)blockIdx.x * (kWG / 64) + wave;
+    const int64_t step = (int64_t)gridDim.x * kWaves;
+    int64_t i = (int64_t)blockIdx.x * kWaves + wave;
     double sum = 0.0;
     Chunk next{};
     const void *g_next = nullptr;
@@ -130,7 +134,26 @@ __global__ __launch_bounds__(kWG) void norm_partial_kernel(const void *chunks, i
         default: sum += chunk_squares<SS_F16>(g, c); break;
         }
     }
-    sum = wg_sum<kWG>(sum);
+    return wg_sum<THREADS>(sum);
+}
+
+__device__ __forceinline__ void write_clip(double sum, double max_norm, double grad_scale,
+                                           float *__restrict__ clip)
+{
+    const double norm = fabs(grad_scale) * sqrt(sum);
+    const bool finite = norm < INFINITY;
+    const double ratio = max_norm / (norm + 1e-6);
+    clip[0] = (float)norm;
+    clip[1] = finite ? (float)(grad_scale * (ratio < 1.0 ? ratio : 1.0)) : 0.0f;
+    clip[2] = finite ? 1.0f : 0.0f;
+    clip[3] = 0.0f;
+}
+
+__global__ __launch_bounds__(kWG) void norm_partial_kernel(const void *chunks, int num_chunks,
+                                                           const void *const *grads,
+                                                           double *__restrict__ part)
+{
+    const double sum = chunks_squares<kWG>(chunks, num_chunks, grads);
     if (threadIdx.x == 0) part[blockIdx.x] = sum;
 }
 
@@ -142,15 +165,18 @@ __global__ __launch_bounds__(kFinalThreads) void norm_final_kernel(const double 
     double sum = 0.0;
     for (int i = threadIdx.x; i < n; i += kFinalThreads) sum += part[i];
     sum = wg_sum<kFinalThreads>(sum);
-    if (threadIdx.x == 0) {
-        const double norm = fabs(grad_scale) * sqrt(sum);
-        const bool finite = norm < INFINITY;
-        const double ratio = max_norm / (norm + 1e-6);
-        clip[0] = (float)norm;
-        clip[1] = finite ? (float)(grad_scale * (ratio < 1.0 ? ratio : 1.0)) : 0.0f;
-        clip[2] = finite ? 1.0f : 0.0f;
-        clip[3] = 0.0f;
-    }
+    if (threadIdx.x == 0) write_clip(sum, max_norm, grad_scale, clip);
+}
+
+__global__ __launch_bounds__(kFinalThreads) void norm_alone_kernel(const void *chunks,
+                                                                   int num_chunks,
+                                                                   const void *const *grads,
+                                                                   double max_norm,
+                                                                   double grad_scale,
+                                                                   float *__restrict__ clip)
+{
+    const double sum = chunks_squares<kFinalThreads>(chunks, num_chunks, grads);
+    if (threadIdx.x == 0) write_clip(sum, max_norm, grad_scale, clip);
 }
 
 // ---- AdamW --------------------------------------------------------------------------------
@@ -734,9 +760,15 @@ int32_t ss_grad_norm(const ss_tensor_list *list, const void *const *grads, doubl
         return fail(SS_ERR_WORKSPACE, "%s: workspace missing, misaligned or under %zu bytes", who,
                     ss_grad_norm_workspace_bytes(list));
     const hipStream_t s = static_cast<hipStream_t>(stream);
+    if (list->num_chunks <= kAloneChunks) {
+        ProfScope prof("norm_alone_kernel", s);
+        launch(norm_alone_kernel, dim3(1), dim3(kFinalThreads), s, list->chunks, list->num_chunks,
+               grads, max_norm, grad_scale, clip);
+        return check_launch(who);
+    }
     const int wgs = norm_wgs(list);
     double *part = static_cast<double *>(ws);
-    if (wgs > 0) {
+    {
         ProfScope prof("norm_partial_kernel", s);
         launch(norm_partial_kernel, dim3(wgs), dim3(kWG), s, list->chunks, list->num_chunks, grads,
                part);

@@ -22,7 +22,8 @@ def norm_of(grads, max_norm, scale=1.0):
 
 @pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16, torch.float16])
 @pytest.mark.parametrize("sizes", [[1], [7, 0, 1], [8192], [8193, 1, 16384, 3], [2_000_003],
-                                   [65] * 700, [50_000] * 500])
+                                   [65] * 700, [50_000] * 500,
+                                   [2048] * 64, [2048] * 65, [131_072], [131_073]])
 def test_norm_and_factor(dtype, sizes):
     gen = torch.Generator(device=DEV).manual_seed(len(sizes) + sizes[0])
     flat = torch.randn(sum(sizes) + 1, device=DEV, generator=gen).to(dtype)[1:]
