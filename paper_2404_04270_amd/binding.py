@@ -989,7 +989,8 @@ def _matrix(who: str, name: str, t: torch.Tensor, like: torch.Tensor, shape):
 
 
 def _rows_args(who: str, x: torch.Tensor, params, mean: torch.Tensor, rstd: torch.Tensor):
-    """Shape, and the types of the matrices and of the parameters (gammas, betas, gradients)."""
+    """Shape, the types of the matrices and of the parameters (gammas, betas, gradients), and the
+    addresses of the parameters, of mean and of rstd."""
     shape, dtype, device = x.shape, x.dtype, x.get_device()
     if len(shape) != 2 or device < 0:
         raise SlipstreamError(f"{who}: x must be a device tensor [rows, dim]")
@@ -998,19 +999,26 @@ def _rows_args(who: str, x: torch.Tensor, params, mean: torch.Tensor, rstd: torc
     if dtype not in DTYPES:
         raise SlipstreamError(f"{who}: {dtype} is not one of fp32, bf16, fp16")
     rows, dim = shape
-    wt = None
+    wt, at = None, []
     for p in params:
-        if p is not None:
-            if wt is None:
-                wt = p.dtype
-                if wt is not dtype and wt is not torch.float32:
-                    raise SlipstreamError(f"{who}: parameters of {wt} (need {dtype} or fp32)")
-            if p.dtype is not wt or p.numel() != dim or p.get_device() != device:
-                raise SlipstreamError(f"{who}: parameters and their gradients need one type and "
-                                      "one element per column")
-    if mean.numel() < rows or rstd.numel() < rows:
-        raise SlipstreamError(f"{who}: mean or rstd is too small")
-    return shape, DTYPES[dtype], dtype if wt is None else wt
+        if p is None:
+            at.append(None)
+            continue
+        if wt is None:
+            wt = p.dtype
+            if wt is not dtype and wt is not torch.float32:
+                raise SlipstreamError(f"{who}: parameters of {wt} (need {dtype} or fp32)")
+        if p.dtype is not wt or p.numel() != dim or p.get_device() != device \
+                or not p.is_contiguous():
+            raise SlipstreamError(f"{who}: parameters and their gradients need one type and one "
+                                  "element per column, contiguous")
+        at.append(p.data_ptr())
+    for t in (mean, rstd):
+        if t.numel() < rows or t.dtype is not torch.float32 or t.get_device() != device \
+                or not t.is_contiguous():
+            raise SlipstreamError(f"{who}: mean and rstd need fp32, contiguous, one element per row")
+        at.append(t.data_ptr())
+    return shape, DTYPES[dtype], DTYPES[dtype if wt is None else wt], device, at
 
 
 def ss_layernorm_rows_forward(x: torch.Tensor, n_valid: Optional[torch.Tensor],
@@ -1019,15 +1027,12 @@ def ss_layernorm_rows_forward(x: torch.Tensor, n_valid: Optional[torch.Tensor],
                               rstd: torch.Tensor, stream=None) -> None:
     """x, y [rows, dim] (rows may be a stride apart); gamma, beta [dim]; mean, rstd fp32 [rows]."""
     who = "ss_layernorm_rows_forward"
-    shape, dt, wt = _rows_args(who, x, (gamma, beta), mean, rstd)
-    on = x.get_device()
+    shape, dt, wt, device, (gp, bp, mp, rp) = _rows_args(who, x, (gamma, beta), mean, rstd)
     xp, xs = _matrix(who, "x", x, x, shape)
     yp, ys = _matrix(who, "y", y, x, shape)
     _check(_lib.ss_layernorm_rows_forward(
-        dt, DTYPES[wt], shape[0], shape[1], xp, xs, _ptr_on(n_valid, torch.int32, "n_valid", on),
-        _ptr(gamma, wt, "gamma"), _ptr(beta, wt, "beta"), eps, yp, ys,
-        _ptr_on(mean, torch.float32, "mean", on), _ptr_on(rstd, torch.float32, "rstd", on),
-        _stream_ptr(stream)))
+        dt, wt, shape[0], shape[1], xp, xs, _ptr_on(n_valid, torch.int32, "n_valid", device), gp, bp,
+        eps, yp, ys, mp, rp, _stream_ptr(stream)))
 
 
 def ss_layernorm_rows_workspace_bytes(rows: int, dim: int) -> int:
@@ -1040,17 +1045,16 @@ def ss_layernorm_rows_backward(dy: torch.Tensor, x: torch.Tensor,
                                dgamma: Optional[torch.Tensor], dbeta: Optional[torch.Tensor],
                                ws: Optional[torch.Tensor], stream=None) -> None:
     who = "ss_layernorm_rows_backward"
-    shape, dt, wt = _rows_args(who, x, (gamma, dgamma, dbeta), mean, rstd)
-    on = x.get_device()
+    shape, dt, wt, device, (gp, dgp, dbp, mp, rp) = _rows_args(who, x, (gamma, dgamma, dbeta), mean,
+                                                               rstd)
     dyp, dys = _matrix(who, "dy", dy, x, shape)
     xp, xs = _matrix(who, "x", x, x, shape)
     dxp, dxs = _matrix(who, "dx", dx, x, shape)
     _check(_lib.ss_layernorm_rows_backward(
-        dt, DTYPES[wt], shape[0], shape[1], dyp, dys, xp, xs,
-        _ptr_on(n_valid, torch.int32, "n_valid", on), _ptr(gamma, wt, "gamma"),
-        _ptr_on(mean, torch.float32, "mean", on), _ptr_on(rstd, torch.float32, "rstd", on), dxp, dxs,
-        _ptr(dgamma, wt, "dgamma"), _ptr(dbeta, wt, "dbeta"), _ptr_on(ws, torch.uint8, "ws", on),
-        0 if ws is None else ws.numel(), _stream_ptr(stream)))
+        dt, wt, shape[0], shape[1], dyp, dys, xp, xs,
+        _ptr_on(n_valid, torch.int32, "n_valid", device), gp, mp, rp, dxp, dxs, dgp, dbp,
+        _ptr_on(ws, torch.uint8, "ws", device), 0 if ws is None else ws.numel(),
+        _stream_ptr(stream)))
 
 
 def stream_handle(stream=None) -> C.c_void_p:

@@ -21,6 +21,8 @@
 namespace ss {
 namespace {
 
+constexpr int kStreamOut = 1, kStreamIn = 2;       // past the caches
+
 // Elements per 16-byte access.
 template <int DT> constexpr int per_access() { return DT == SS_F32 ? 4 : 8; }
 
@@ -96,13 +98,18 @@ template <int LANES, int N> struct Columns {
     }
 };
 
+// Between the two sides of a branch that differ in nothing but the cache policy of an access: the
+// compiler would make one access of them, and take the policy of neither.
+__device__ __forceinline__ void apart() { asm volatile(""); }
+
 // Zeros past the row.  The last vector of a row that is no multiple of N is read where it ends with the
 // row (there is room for that: a row of several lanes is longer than N) and shifted down: one load
 // for a lane where elements taken one by one would cost its whole wavefront N.  The shift is a step
 // of its own, so that asking for a row does not wait for it.
 template <int DT, int LANES, int N>
 __device__ __forceinline__ Raw<DT, N> ask_columns(const void *base, int64_t row,
-                                                  const Columns<LANES, N> &at)
+                                                  const Columns<LANES, N> &at,
+                                                  bool stream = false)
 {
     if constexpr (LANES == 1) {
         if (at.count < N) return load_raw_part<DT, N>(base, row + at.col, at.count);
@@ -110,7 +117,16 @@ __device__ __forceinline__ Raw<DT, N> ask_columns(const void *base, int64_t row,
     }
     Raw<DT, N> r;
     r.v = 0.0f;
-    if (at.count > 0) r = load_raw<DT, N>(base, row + at.col + at.count - N);
+    if (at.count > 0) {
+        const int64_t from = row + at.col + at.count - N;
+        if (stream) {
+            apart();
+            r = load_raw<DT, N, true>(base, from);
+            apart();
+        } else {
+            r = load_raw<DT, N>(base, from);
+        }
+    }
     return r;
 }
 template <int DT, int LANES, int N>
@@ -151,11 +167,17 @@ __device__ __forceinline__ void store_rest(void *base, int64_t at, int n, const 
 // A row's rest of fewer than N columns: in up to log2(N) stores.
 template <int DT, int LANES, int N>
 __device__ __forceinline__ void store_columns(void *base, int64_t row, const Columns<LANES, N> &at,
-                                              const float (&f)[N])
+                                              const float (&f)[N], bool stream = false)
 {
     const Raw<DT, N> r = from_float<DT, N>(f);
     if (at.count == N) {
-        store_raw<DT, N>(base, row + at.col, r);
+        if (stream) {
+            apart();
+            store_raw<DT, N, true>(base, row + at.col, r);
+            apart();
+        } else {
+            store_raw<DT, N>(base, row + at.col, r);
+        }
     } else if (at.count > 0) {
         if constexpr (N == 8) {
             Raw<DT, 4> four;
@@ -205,7 +227,7 @@ template <int DT, int WT, int LANES, int P>
 __global__ __launch_bounds__(fwd_threads<LANES>()) void rows_forward_kernel(
     const void *x, int64_t x_stride, int rows, const int32_t *__restrict__ n_valid,
     const void *gamma, const void *beta, float eps, void *y, int64_t y_stride,
-    float *__restrict__ mean, float *__restrict__ rstd, int dim)
+    float *__restrict__ mean, float *__restrict__ rstd, int dim, int flow)
 {
     constexpr int N = per_access<DT>(), T = fwd_threads<LANES>(), NG = T / LANES;
     __shared__ float s[2][LANES > 64 ? T / 64 : 1];
@@ -218,7 +240,7 @@ __global__ __launch_bounds__(fwd_threads<LANES>()) void rows_forward_kernel(
     const auto ask = [&] {
 #pragma unroll
         for (int i = 0; i < P; ++i)
-            raw[i] = ask_columns<DT>(x, x_at, Columns<LANES, N>(i, c, dim));
+            raw[i] = ask_columns<DT>(x, x_at, Columns<LANES, N>(i, c, dim), flow & kStreamIn);
     };
     if (r < n) ask();
     float gam[P][N], bet[P][N];
@@ -256,7 +278,7 @@ __global__ __launch_bounds__(fwd_threads<LANES>()) void rows_forward_kernel(
             float o[N];
 #pragma unroll
             for (int e = 0; e < N; ++e) o[e] = fmaf(v[i][e] * rs, gam[i][e], bet[i][e]);
-            store_columns<DT>(y, y_at, Columns<LANES, N>(i, c, dim), o);
+            store_columns<DT>(y, y_at, Columns<LANES, N>(i, c, dim), o, flow & kStreamOut);
         }
         if (c == 0) {
             mean[r] = mu;
@@ -271,13 +293,14 @@ template <bool FIRST, typename A, typename B> __device__ __forceinline__ auto &p
     else return b;
 }
 
-// part: [2][gridDim.x][dim], the products' sums and the gradients' sums; may be null.
+// part: [2][gridDim.x][dim], the products' sums and the gradients' sums.  A workgroup that is alone
+// writes dgamma and dbeta itself and needs no part.
 template <int DT, int WT, int LANES, int P>
 __global__ __launch_bounds__(bwd_threads<LANES>()) void rows_backward_kernel(
     const void *dy, int64_t dy_stride, const void *x, int64_t x_stride, int rows,
     const int32_t *__restrict__ n_valid, const void *gamma, const float *__restrict__ mean,
-    const float *__restrict__ rstd, void *dx, int64_t dx_stride, int dim,
-    float *__restrict__ part)
+    const float *__restrict__ rstd, void *dx, int64_t dx_stride, int dim, int flow,
+    float *__restrict__ part, void *dgamma, void *dbeta)
 {
     constexpr int N = per_access<DT>(), T = bwd_threads<LANES>(), NG = T / LANES;
     // a lane with 32 elements has no registers left for gamma and the next row
@@ -295,8 +318,8 @@ __global__ __launch_bounds__(bwd_threads<LANES>()) void rows_backward_kernel(
 #pragma unroll
         for (int i = 0; i < P; ++i) {
             const Columns<LANES, N> at(i, c, dim);
-            xn[i] = ask_columns<DT>(x, x_at, at);
-            dn[i] = ask_columns<DT>(dy, dy_at, at);
+            xn[i] = ask_columns<DT>(x, x_at, at, kKeep && flow & kStreamIn);
+            dn[i] = ask_columns<DT>(dy, dy_at, at, kKeep && flow & kStreamIn);
         }
         mu_n = mean[row];
         rs_n = rstd[row];
@@ -368,15 +391,17 @@ __global__ __launch_bounds__(bwd_threads<LANES>()) void rows_backward_kernel(
 #pragma unroll
                 for (int e = 0; e < N; ++e)
                     o[e] = fmaf((mu - xf[e]) * rs, m2, fmaf(df[e], gm[e], -m1)) * rs;
-                store_columns<DT>(dx, dx_at, Columns<LANES, N>(i, c, dim), o);
+                store_columns<DT>(dx, dx_at, Columns<LANES, N>(i, c, dim), o, flow & kStreamOut);
                 if (!kKeep) __builtin_amdgcn_sched_barrier(0);
             }
         }
         dx_at += step * dx_stride;
     }
-    if (!part) return;
+    if (!dgamma && !dbeta) return;
 #pragma unroll
     for (int which = 0; which < 2; ++which) {
+        void *const own = which ? dbeta : dgamma;
+        if (!own) continue;
         float *out = part + ((int64_t)which * gridDim.x + blockIdx.x) * dim;
 #pragma unroll
         for (int i = 0; i < P; ++i) {
@@ -395,8 +420,12 @@ __global__ __launch_bounds__(bwd_threads<LANES>()) void rows_backward_kernel(
                     if (col >= dim) break;
                     float sum = 0.0f;
                     for (int o = 0; o < NG; ++o) sum += s_col[j % N * T + o * LANES + j / N];
-                    out[col] = sum;
+                    typedef typename ElemOf<WT>::type W;
+                    if (gridDim.x == 1) static_cast<W *>(own)[col] = (W)sum;
+                    else out[col] = sum;
                 }
+            } else if (gridDim.x == 1) {
+                store_columns<WT>(own, 0, at, t);
             } else {
                 store_columns<SS_F32>(out, 0, at, t);
             }
@@ -669,6 +698,24 @@ constexpr int kWideWgs = 1024;
 // fp32 71 and 81.  Elsewhere the second adds partial rows and nothing else: 32768 x 4096 bf16 157 and
 // 150, 2048 x 4096 19.6 and 17.2, 16384 x 1024 29.3 and 24.4.
 constexpr int kBackwardWgs = 256;
+// Up to so many rows per group of lanes one workgroup takes them all, and there is no second launch:
+// 128 x 64 fp32 9.8 instead of 11.7 us from call to call, 32 x 1024 bf16 9.9 and 12.0.
+constexpr int kAloneRows = 4;
+
+// What goes past the caches.  Results do from 32 MB on, where none of them would stay in the L2s (below,
+// whoever reads them next would lose), if their rows start at even places: 65536 x 512 fp16 forward
+// 26.1 -> 22.7 us, 16384 x 2048 bf16 26.2 -> 22.9, 32768 x 4096 bf16 backward 150 -> 146 (odd places:
+// 10007 x 1001 fp32 forward 13.3 -> 14.9).  What is read does from 256 MB in all on, which is more
+// than the last-level cache: 32768 x 4096 bf16 backward 146 -> 140, 16384 x 4096 fp32 152 -> 140, 16384 x
+// 8192 bf16 forward 94 -> 92 (16384 x 2048 forward, 134 MB, 22.9 -> 25.7).
+int flow_of(int rows, int dim, int dtype, const void *out, int64_t out_stride, int arrays)
+{
+    const int size = dtype == SS_F32 ? 4 : 2;
+    const int64_t bytes = (int64_t)rows * dim * size;
+    const bool even = ((reinterpret_cast<uintptr_t>(out) | (uintptr_t)(out_stride * size)) & 15) == 0;
+    return (bytes >= 32 << 20 && even ? kStreamOut : 0) |
+           (bytes * arrays >= 256 << 20 ? kStreamIn : 0);
+}
 
 int32_t check_rows(const char *who, int32_t dtype, int32_t param_dtype, int32_t rows, int32_t dim)
 {
@@ -722,6 +769,7 @@ int32_t ss_layernorm_rows_forward(int32_t dtype, int32_t param_dtype, int32_t ro
     if (rows == 0) return SS_OK;
     const hipStream_t st = static_cast<hipStream_t>(stream);
     const Shape sh = shape_of(dim, dtype == SS_F32 ? 4 : 8);
+    const int flow = flow_of(rows, dim, dtype, y, y_stride, 2);
     ProfScope prof("rows_forward_kernel", st);
 #define SS_ROWS_FWD                                                                           \
     const int threads = fwd_threads<LANES>();                                                 \
@@ -729,7 +777,7 @@ int32_t ss_layernorm_rows_forward(int32_t dtype, int32_t param_dtype, int32_t ro
     const int64_t most = kForwardThreads / threads;                                           \
     launch(rows_forward_kernel<DT, WT, LANES, P>, dim3((unsigned)(need < most ? need : most)),\
            dim3(threads), st, x, x_stride, rows, n_valid, gamma, beta, eps, y, y_stride, mean,\
-           rstd, dim)
+           rstd, dim, flow)
     SS_ROWS_TYPES(dtype, param_dtype,
                   SS_ROWS_SHAPES(SS_ROWS_FWD) else launch(
                       wide_forward_kernel<DT, WT>, dim3(rows < kWideWgs ? rows : kWideWgs),
@@ -773,6 +821,7 @@ int32_t ss_layernorm_rows_backward(int32_t dtype, int32_t param_dtype, int32_t r
     const hipStream_t st = static_cast<hipStream_t>(stream);
     const int per = dtype == SS_F32 ? 4 : 8;
     const Shape sh = shape_of(dim, per);
+    const int flow = flow_of(rows, dim, dtype, dx, dx_stride, 3);
     float *part = params ? static_cast<float *>(ws) : nullptr;
     int n_part = 0;
     if (rows > 0) {
@@ -782,11 +831,11 @@ int32_t ss_layernorm_rows_backward(int32_t dtype, int32_t param_dtype, int32_t r
     const int64_t groups = threads / LANES, need = (rows + groups - 1) / groups;              \
     n_part = (int)(need < most ? need : most);                                                \
     const int wgs = P > 1 ? kBackwardWgs : 2 * kBackwardWgs;                                  \
-    n_part = n_part < wgs ? n_part : wgs;                                                     \
+    n_part = need <= kAloneRows ? 1 : n_part < wgs ? n_part : wgs;                            \
     ProfScope prof("rows_backward_kernel", st);                                               \
     launch(rows_backward_kernel<DT, WT, LANES, P>, dim3(n_part), dim3(threads), st, dy,       \
            dy_stride, x, x_stride, rows, n_valid, gamma, mean, rstd, dx, dx_stride, dim,      \
-           part)
+           flow, part, dgamma, dbeta)
 #define SS_ROWS_WIDE                                                                          \
     if (params) {                    /* first: dx may be dy or x */                           \
         n_part = most;                                                                        \
@@ -803,7 +852,7 @@ int32_t ss_layernorm_rows_backward(int32_t dtype, int32_t param_dtype, int32_t r
 #undef SS_ROWS_BWD
 #undef SS_ROWS_WIDE
     }
-    if (params) {
+    if (params && !(sh.lanes > 0 && n_part == 1)) {
         ProfScope prof("columns_reduce_kernel", st);
         const dim3 grid((dim + kRedCols - 1) / kRedCols, 2);
         SS_ROWS_TYPES(param_dtype, param_dtype,

@@ -113,6 +113,12 @@ def test_every_split_of_a_row(dim, dtype, wt):
     (1, 1, BF16, BF16, 0, None), (1, 4096, BF16, BF16, 0, None), (3, 100_000, F32, F32, 3, None),
     (3, 100_000, BF16, BF16, 0, 2), (7, 64, F32, F32, 0, 0), (2, 20_000, F16, F32, 0, 0),
     (300, 40, F16, F32, 24, 299), (5000, 13, F32, F32, 0, 4999), (70_001, 8, BF16, F32, 0, None),
+    # one workgroup takes all rows (4 per group of lanes) and just not; results past the caches from 32 MB
+    # on, inputs from 256 MB on
+    (128, 64, F32, F32, 0, None), (129, 64, F32, F32, 0, None), (32, 1000, BF16, BF16, 1, 31),
+    (33, 1000, BF16, F32, 0, None), (4, 8192, F16, F16, 0, 3), (3, 16384, BF16, F32, 0, None),
+    (16400, 1024, BF16, BF16, 0, 16399), (16400, 1023, F32, F32, 1, None),
+    (22000, 2048, F32, F32, 0, None), (45001, 2047, F16, F16, 0, 45000),
     (2500, 512, BF16, BF16, 5, 2047), (3001, 1024, F32, F32, 0, None), (1500, 6000, F16, F16, 1, 1499)])
 def test_rows_strides_and_valid_counts(rows, dim, dtype, wt, pad, n_valid):
     both_ways(rows, dim, dtype, wt, pad, n_valid, seed=rows + dim)
