@@ -854,11 +854,10 @@ class TensorList:
         self.starts = starts
         self._pptr = _ptr_table(self.params, self.device)
         self.grads: Optional[List[torch.Tensor]] = None
-        self._gptr: Optional[torch.Tensor] = None
         if grads is not None:
             self._check_grads(list(grads))
             self.grads = list(grads)
-            self._gptr = _ptr_table(self.grads, self.device)
+        self._gptr = _ptr_table(self.params if grads is None else self.grads, self.device)
 
     def _check_grads(self, grads) -> List[int]:
         if len(grads) != len(self.params):
@@ -874,10 +873,7 @@ class TensorList:
         """The gradients that the calls after this one read, in order on the stream.  Under capture
         the addresses become part of the graph."""
         _here(self.device, "set_grads")
-        ptrs = self._check_grads(grads)
-        if self._gptr is None:
-            self._gptr = torch.empty(len(ptrs), dtype=torch.int64, device=self.device)
-        ss_pointer_table(self._gptr, ptrs, stream)
+        ss_pointer_table(self._gptr, self._check_grads(grads), stream)
         self.grads = list(grads)
 
     def of(self, flat: torch.Tensor, k: int) -> torch.Tensor:
@@ -897,7 +893,7 @@ def ss_grad_norm(tensors: TensorList, max_norm: float, clip: torch.Tensor, ws: t
                  grad_scale: float = 1.0, stream=None) -> None:
     """clip fp32 [4]: norm, clip factor, 1 where the norm is finite, 0."""
     _here(tensors.device, "ss_grad_norm")
-    if tensors._gptr is None:
+    if tensors.grads is None:
         raise SlipstreamError("ss_grad_norm: the list has no gradients yet (set_grads)")
     if clip.numel() < 4:
         raise SlipstreamError("ss_grad_norm: clip needs four floats")
@@ -943,7 +939,7 @@ def ss_adamw_step(tensors: TensorList, state: AdamWState, lr, beta1: float = 0.9
                   clip: Optional[torch.Tensor] = None, stream=None) -> None:
     """lr: a number, or a device tensor of one float that is read when the step runs."""
     _here(tensors.device, "ss_adamw_step")
-    if tensors._gptr is None or tensors.only_grads:
+    if tensors.grads is None or tensors.only_grads:
         raise SlipstreamError("ss_adamw_step: the list has no gradients yet (set_grads), or holds "
                               "nothing else")
     if state.m.numel() != tensors.state_elems or state.m.device != tensors.device:

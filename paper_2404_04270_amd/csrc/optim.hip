@@ -315,7 +315,7 @@ template <int P, int G, bool MASTER> struct Four {
 };
 
 // How a chunk is read and written: through the caches, past them, or past them but for parameters
-// and gradients (whose accesses share cache lines where a tensor starts at an odd place).
+// and gradients (whose narrow accesses share cache lines where a tensor starts at an odd place).
 enum Flow { kCached, kStream, kStreamMoments };
 
 template <Flow F> __device__ __forceinline__ f4 load_moments(const float *p)
@@ -438,8 +438,10 @@ __global__ __launch_bounds__(kWG) void adamw_kernel(const void *chunks, void *co
         if (SOLO) end_solo(scalars, s);
         return;
     }
+    // 16 bits at odd places: 20 M bf16 elements with master copies 92 instead of 103 us; fp32 does not
+    // mind them (2^28 elements at odd places 1333 past the caches, 1338 to 1354 otherwise)
     const bool even = ((reinterpret_cast<uintptr_t>(at.p) | reinterpret_cast<uintptr_t>(at.g)) &
-                       15) == 0;
+                       15) == 0 || (c.kind & 15) == (SS_F32 | SS_F32 << 2);
     if (!STREAM) {
         SS_DISPATCH_KIND(c.kind, master != nullptr,
                          step_chunk<kCached, P, G, MASTER>(at, c.count, k, s, keep));

@@ -11,9 +11,9 @@
 // workgroup goes to memory, and a second kernel adds those in order.
 //
 // us, and TB/s of x, y, dy and dx (a device-wide addition of a constant reaches 6.2): forward
-// 16384 x 8192 bf16 95 (5.6), 65536 x 512 fp16 26 (5.2), 10007 x 1001 fp32 13.3 (6.0, partly from the
-// last-level cache); backward 32768 x 4096 bf16 150 (5.4), 16384 x 4096 fp32 155 (5.2),
-// 16384 x 1024 bf16 24.6 (4.1), 10007 x 1001 fp16 17.9 (3.4), each with about 4 us for the second
+// 16384 x 8192 bf16 89 (6.1), 65536 x 512 fp16 22.7 (5.9), 10007 x 1001 fp32 13.3 (6.0, partly from the
+// last-level cache); backward 32768 x 4096 bf16 139 (5.8), 16384 x 4096 fp32 139 (5.8),
+// 16384 x 1024 bf16 22.2 (4.5), 10007 x 1001 fp16 18 (3.4), each with about 4 us for the second
 // kernel.
 #include "elem_io.h"
 #include "ss_common.h"
