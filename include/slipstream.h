@@ -460,6 +460,7 @@ enum { SS_F32 = 0, SS_BF16 = 1, SS_F16 = 2 };
  */
 #define SS_MOMENT_BLOCK 128
 #define SS_CHUNK_BYTES 32
+#define SS_ADAMW_COUNTER_BYTES 2112
 typedef struct {
     int64_t numel;       /* >= 0 */
     int32_t dtype;       /* of the parameter: SS_F32, SS_BF16 or SS_F16 */
@@ -509,9 +510,10 @@ int32_t ss_grad_norm(const ss_tensor_list *list, const void *const *grads, doubl
  *             8: m and v are uint8 [state_elems], exps is uint8 [state_elems / SS_MOMENT_BLOCK][2];
  *             see below
  *   master    float [state_elems] or NULL; used for the tensors of 16 bits
- *   counters  64 bytes, 64-byte aligned, zeroed before the first step: int64 steps taken, int64
- *             steps left out, and the scalars of the step in progress.  A step counts itself on
- *             the device, so that it can be captured in a graph and replayed.
+ *   counters  SS_ADAMW_COUNTER_BYTES, 64-byte aligned, zeroed before the first step: int64 steps
+ *             taken, int64 steps left out, and what belongs to the step in progress.  A step
+ *             counts itself on the device, so that it can be captured in a graph and replayed;
+ *             two steps of one state must not overlap.
  * m, v, exps and master are 16-byte aligned.  All zeros is the state before the first step, in
  * either form.
  *

@@ -778,6 +778,7 @@ def ss_embbag_ln_backward(tables: Tables, idx: torch.Tensor, n_valid: Optional[t
 
 DTYPES = {torch.float32: 0, torch.bfloat16: 1, torch.float16: 2}
 MOMENT_BLOCK = 128
+COUNTER_BYTES = 2112
 
 
 def _here(device: torch.device, who: str) -> None:
@@ -927,7 +928,7 @@ class AdamWState:
             self.master = torch.zeros(n, device=dev)
             torch._foreach_copy_([tensors.of(self.master, k) for k in range(len(tensors.params))],
                                  [p.detach().reshape(-1) for p in tensors.params])
-        self.counters = torch.zeros(8, dtype=torch.int64, device=dev)
+        self.counters = torch.zeros(COUNTER_BYTES // 8, dtype=torch.int64, device=dev)
         self.c = _CAdamWState(
             bits, 0, self.m.data_ptr(), self.v.data_ptr(),
             None if self.exps is None else self.exps.data_ptr(),

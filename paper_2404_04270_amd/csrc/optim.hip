@@ -189,10 +189,18 @@ struct Scalars {
     float factor;              // of the gradients
     uint32_t dither;           // of element 0
     int32_t apply;
-    uint32_t ended;            // workgroups of the present step that have ended
+    uint32_t lines_ended;      // lines below whose workgroups have all ended
     int32_t reserved[5];
 };
-static_assert(sizeof(Scalars) == 64, "the header says how large the counters are");
+// A cache line for every kEndLines-th workgroup of a step that tells its own end (below).
+constexpr int kEndLines = 32;
+struct Counters {
+    Scalars scalars;
+    struct {
+        uint32_t ended, reserved[15];
+    } line[kEndLines];
+};
+static_assert(sizeof(Counters) == SS_ADAMW_COUNTER_BYTES, "the header says how large they are");
 
 constexpr uint32_t kDitherElement = 0x6A09E667u;   // the fraction of sqrt(2)
 constexpr uint32_t kDitherStep = 0x9E3779B9u;      // the golden ratio
@@ -234,16 +242,18 @@ __global__ __launch_bounds__(64) void adamw_begin_kernel(Scalars *scalars, Begin
 {
     if (threadIdx.x != 0) return;
     Scalars s = begin_step(scalars, b);
-    s.ended = 0;
+    s.lines_ended = 0;
     *scalars = s;
 }
 
 // A step of few workgroups has one launch: each works out the scalars for itself, and the last to end
-// counts the step (nobody waits: all have read the count by then).  A workgroup's turn at the
-// counter that tells the last takes about 16 ns: us per fp32 step of 60 / 140 / 260 / 380 / 500 chunks in
-// one launch and in two 5.2 / 5.2 / 6.9 / 9.0 / 11.5 and 7.5 / 8.1 / 7.7 / 7.7 / 8.5 (packed moments
-// 4.9 / - / 7.0 / - / 10.0 and 7.2 / - / 7.8 / - / 7.7).
-constexpr int kSoloChunks = 288;
+// counts the step (nobody waits: all have read the count by then).  A workgroup's turn at a counter
+// takes about 16 ns, so they count themselves on kEndLines counters first, and the last of each there
+// on one.  us per fp32 step of 60 / 260 / 380 / 500 / 1000 / 2000 chunks in one launch and in two 5.6 /
+// 5.5 / 6.4 / 7.8 / 11.1 / 19.2 and 9.0 / 8.0 / 7.9 / 8.6 / 11.9 / 20.1 (on a single counter 5.2 / 6.9 /
+// 9.0 / 11.5 / 19.5 / 32.1); packed moments 5.3 / 5.6 / - / 6.1 / 8.0 / 12.7 and 7.5 / 7.9 / - / 7.9 /
+// 8.7 / 12.3.
+constexpr int kSoloChunks = 1024;
 
 __device__ __forceinline__ int32_t uniform(int32_t x) { return __builtin_amdgcn_readfirstlane(x); }
 __device__ __forceinline__ float uniform(float x) { return __int_as_float(uniform(__float_as_int(x))); }
@@ -267,17 +277,24 @@ __device__ __forceinline__ Scalars begin_solo(const Scalars *scalars, const Begi
     return s;
 }
 
-__device__ __forceinline__ void end_solo(Scalars *scalars, const Scalars &s)
+__device__ __forceinline__ bool last_of(uint32_t *counter, uint32_t n)
+{
+    const uint32_t before = __hip_atomic_fetch_add(counter, 1u, __ATOMIC_RELAXED,
+                                                   __HIP_MEMORY_SCOPE_AGENT);
+    if (before + 1 != n) return false;
+    *counter = 0;              // for the next step
+    return true;
+}
+
+__device__ __forceinline__ void end_solo(Counters *c, const Scalars &s)
 {
     __syncthreads();           // every wavefront has used the count it read
     if (threadIdx.x != 0) return;
-    const unsigned before = __hip_atomic_fetch_add(&scalars->ended, 1u, __ATOMIC_RELAXED,
-                                                   __HIP_MEMORY_SCOPE_AGENT);
-    if (before + 1 == gridDim.x) {
-        scalars->steps = s.steps;
-        scalars->left_out = s.left_out;
-        scalars->ended = 0;
-    }
+    const uint32_t line = blockIdx.x % kEndLines, n = gridDim.x;
+    if (!last_of(&c->line[line].ended, (n - line - 1) / kEndLines + 1)) return;
+    if (!last_of(&c->scalars.lines_ended, n < kEndLines ? n : kEndLines)) return;
+    c->scalars.steps = s.steps;
+    c->scalars.left_out = s.left_out;
 }
 
 struct Betas {
@@ -427,15 +444,15 @@ constexpr int64_t kStreamElems = 8 << 20;
 template <bool STREAM, bool SOLO>
 __global__ __launch_bounds__(kWG) void adamw_kernel(const void *chunks, void *const *params,
                                                     const void *const *grads, float *m, float *v,
-                                                    float *master, Scalars *scalars, Betas k,
+                                                    float *master, Counters *counters, Betas k,
                                                     Begin b)
 {
     const Chunk c = load_chunk(chunks, chunk_of_block());
-    const Scalars s = SOLO ? begin_solo(scalars, b) : *scalars;
+    const Scalars s = SOLO ? begin_solo(&counters->scalars, b) : counters->scalars;
     const Places at{params[c.tensor], grads[c.tensor], m, v, master, c.first, c.state};
     const float keep = c.kind & 16 ? 1.0f : s.keep;
     if (!s.apply) {
-        if (SOLO) end_solo(scalars, s);
+        if (SOLO) end_solo(counters, s);
         return;
     }
     // 16 bits at odd places: 20 M bf16 elements with master copies 92 instead of 103 us; fp32 does not
@@ -452,7 +469,7 @@ __global__ __launch_bounds__(kWG) void adamw_kernel(const void *chunks, void *co
         SS_DISPATCH_KIND(c.kind, master != nullptr,
                          step_chunk<kStreamMoments, P, G, MASTER>(at, c.count, k, s, keep));
     }
-    if (SOLO) end_solo(scalars, s);
+    if (SOLO) end_solo(counters, s);
 }
 
 // ---- AdamW with moments in 8 bits -----------------------------------------------------------
@@ -611,11 +628,11 @@ template <bool SOLO, bool EXACT>
 __global__ __launch_bounds__(kWG) void adamw_packed_kernel(const void *chunks, void *const *params,
                                                            const void *const *grads, uint8_t *m,
                                                            uint8_t *v, uint8_t *exps,
-                                                           float *master, Scalars *scalars,
+                                                           float *master, Counters *counters,
                                                            Betas k, Begin b)
 {
     const Chunk c = load_chunk(chunks, chunk_of_block());
-    const Scalars s = SOLO ? begin_solo(scalars, b) : *scalars;
+    const Scalars s = SOLO ? begin_solo(&counters->scalars, b) : counters->scalars;
     void *p = params[c.tensor];
     const void *g = grads[c.tensor];
     const float keep = c.kind & 16 ? 1.0f : s.keep;
@@ -623,7 +640,7 @@ __global__ __launch_bounds__(kWG) void adamw_packed_kernel(const void *chunks, v
         SS_DISPATCH_KIND(c.kind, master != nullptr,
                          step_chunk8<EXACT, P, G, MASTER>(c, p, g, m, v, exps, master, k, s, keep));
     }
-    if (SOLO) end_solo(scalars, s);
+    if (SOLO) end_solo(counters, s);
 }
 
 // The values that packed moments stand for: 8 elements per lane.
@@ -805,7 +822,7 @@ int32_t ss_adamw_step(const ss_tensor_list *list, void *const *params, const voi
     if (!(eps >= 1e-30 && eps <= 1e30))
         return fail(SS_ERR_INVALID_ARG, "%s: eps = %g (need 1e-30 to 1e30)", who, eps);
     const hipStream_t s = static_cast<hipStream_t>(stream);
-    Scalars *scalars = static_cast<Scalars *>(state->counters);
+    Counters *counters = static_cast<Counters *>(state->counters);
     const Betas k{(float)beta1, (float)(1.0 - beta1), (float)beta2, (float)(1.0 - beta2),
                   (float)eps};
     const Begin b{lr, log(beta1), log(beta2), weight_decay, lr_device, clip};
@@ -813,7 +830,7 @@ int32_t ss_adamw_step(const ss_tensor_list *list, void *const *params, const voi
     const bool solo = list->num_chunks > 0 && list->num_chunks <= kSoloChunks;
     if (!solo) {
         ProfScope prof("adamw_begin_kernel", s);
-        launch(adamw_begin_kernel, dim3(1), dim3(64), s, scalars, b);
+        launch(adamw_begin_kernel, dim3(1), dim3(64), s, &counters->scalars, b);
     }
     if (list->num_chunks > 0 && state->bits == 32) {
         ProfScope prof("adamw_kernel", s);
@@ -821,7 +838,7 @@ int32_t ss_adamw_step(const ss_tensor_list *list, void *const *params, const voi
                     : list->state_elems >= kStreamElems ? adamw_kernel<true, false>
                                                         : adamw_kernel<false, false>,
                grid, dim3(kWG), s, list->chunks, params, grads, static_cast<float *>(state->m),
-               static_cast<float *>(state->v), state->master, scalars, k, b);
+               static_cast<float *>(state->v), state->master, counters, k, b);
     } else if (list->num_chunks > 0) {
         ProfScope prof("adamw_packed_kernel", s);
         const bool exact = eps < kLeastFastEps;
@@ -829,7 +846,7 @@ int32_t ss_adamw_step(const ss_tensor_list *list, void *const *params, const voi
                : solo ? adamw_packed_kernel<true, false> : adamw_packed_kernel<false, false>,
                grid, dim3(kWG), s, list->chunks, params, grads,
                static_cast<uint8_t *>(state->m), static_cast<uint8_t *>(state->v), state->exps,
-               state->master, scalars, k, b);
+               state->master, counters, k, b);
     }
     return check_launch(who);
 }

@@ -23,10 +23,11 @@ def reference(p, g, m, v, t, **kw):
     return ref.adamw(p, g, m, v, t, **kw)
 
 
-# 288 chunks of 2048 elements and fewer go in one launch; from 8 M elements on a step streams
+# 1024 chunks of 2048 elements and fewer go in one launch; from 8 M elements on a step streams
 @pytest.mark.parametrize("dtype,grad_dtype,master", [
     (F32, F32, False), (BF16, BF16, True), (BF16, F32, False), (F16, F16, False), (F16, F32, True)])
-@pytest.mark.parametrize("sizes,odd", [([600_000, 1, 4097, 2048], 1), ([289 * 2048], 0),
+@pytest.mark.parametrize("sizes,odd", [([600_000, 1, 4097, 2048], 1), ([1024 * 2048], 0),
+                                       ([1024 * 2048 + 1], 0), ([33 * 2048], 0),
                                        ([8_400_000, 2048, 77], 0), ([5_000_001, 3_500_000], 1)])
 def test_steps_of_larger_lists(sizes, odd, dtype, grad_dtype, master):
     from paper_2404_04270_amd import AdamW
@@ -64,7 +65,7 @@ def test_one_launch_and_two_agree(bits):
     first = tensors([500_001], F32, 3, 0.05, 0)[0]
     grad = tensors([500_001], F32, 4, 1e-2, 0)[0]
     results = []
-    for more in (0, 300_000, 9_000_000):
+    for more in (0, 1_700_000, 9_000_000):
         ps = [first.clone()] + tensors([more], F32, 5, 0.05, 0)
         gs = [grad] + tensors([more], F32, 6, 1e-2, 0)
         opt = AdamW(ps, state_bits=bits)
@@ -80,7 +81,7 @@ def test_one_launch_and_two_agree(bits):
 
 def test_large_list_steps_out_of_a_graph_and_is_left_out():
     from paper_2404_04270_amd import AdamW
-    ps, gs = tensors([700_000, 513], BF16, 7, 0.05, 0), tensors([700_000, 513], BF16, 8, 1e-2, 0)
+    ps, gs = tensors([2_200_000, 513], BF16, 7, 0.05, 0), tensors([2_200_000, 513], BF16, 8, 1e-2, 0)
     twin = [p.clone() for p in ps]
     opts = [AdamW(x, state_bits=8, max_norm=0.5) for x in (ps, twin)]
     for o in opts:
