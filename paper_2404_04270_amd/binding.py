@@ -797,6 +797,11 @@ def _ptr_on(t: Optional[torch.Tensor], dtype, name: str, index: int):
     return _ptr(t, dtype, name)
 
 
+def _stream_on(stream, index: int):
+    """Handle of `stream`, or of the current stream of device `index`, where tensors are already."""
+    return torch._C._cuda_getCurrentRawStream(index) if stream is None else stream.cuda_stream
+
+
 class TensorList:
     """The tensors of a model (contiguous, fp32 / bf16 / fp16, views at any place of a buffer among
     them), with the work table and the pointer arrays that ss_grad_norm and ss_adamw_step read.
@@ -815,59 +820,71 @@ class TensorList:
         if n == 0:
             raise SlipstreamError("TensorList: no tensors")
         self.device = self.params[0].device
-        for p in self.params:
-            if p.dtype not in DTYPES:
-                raise SlipstreamError(f"TensorList: {p.dtype} is not one of fp32, bf16, fp16")
-            _dev_ptr(p, p.dtype, "params")
-            if p.device != self.device:
+        index = self.params[0].get_device()
+        dtypes = [p.dtype for p in self.params]
+        for p, d in zip(self.params, dtypes):
+            if d not in DTYPES:
+                raise SlipstreamError(f"TensorList: {d} is not one of fp32, bf16, fp16")
+            if not p.is_cuda or not p.is_contiguous():
+                _dev_ptr(p, d, "params")         # raises
+            if p.get_device() != index:
                 raise SlipstreamError("TensorList: the tensors are on several devices")
+        numels = [p.numel() for p in self.params]
+        at = [p.data_ptr() for p in self.params]
         self.only_grads = grads is None and grad_dtypes is None
         if self.only_grads:
             grads = self.params
         else:                                    # a step writes them: each element belongs to one
-            spans = sorted((p.data_ptr(), p.data_ptr() + p.numel() * p.element_size())
-                           for p in self.params if p.numel())
+            spans = sorted((a, a + k * d.itemsize) for a, k, d in zip(at, numels, dtypes) if k)
             if any(a[1] > b[0] for a, b in zip(spans, spans[1:])):
                 raise SlipstreamError("TensorList: two parameters overlap, or one is there twice")
+        if grads is not None:
+            grads = list(grads)
         if grad_dtypes is None:
             grad_dtypes = [g.dtype for g in grads]
         self.grad_dtypes = list(grad_dtypes)
         no_decay = [False] * n if no_decay is None else list(no_decay)
         if len(self.grad_dtypes) != n or len(no_decay) != n:
             raise SlipstreamError("TensorList: one gradient type and one no_decay per tensor")
-        for p, d in zip(self.params, self.grad_dtypes):
-            if d not in (p.dtype, torch.float32):
-                raise SlipstreamError(f"TensorList: gradients of {d} for a parameter of {p.dtype}")
+        for p, d in zip(dtypes, self.grad_dtypes):
+            if d is not p and d is not torch.float32:
+                raise SlipstreamError(f"TensorList: gradients of {d} for a parameter of {p}")
+        self._grad_facts = list(zip(self.grad_dtypes, numels))
         tensors = (_CTensor * n)(*[
-            (p.numel(), DTYPES[p.dtype], DTYPES[d], int(bool(k)), 0)
-            for p, d, k in zip(self.params, self.grad_dtypes, no_decay)])
+            (k, DTYPES[p], DTYPES[d], 1 if out else 0, 0)
+            for k, p, d, out in zip(numels, dtypes, self.grad_dtypes, no_decay)])
         self.c = _CTensorList()
         _check(_lib.ss_tensor_list_plan(tensors, n, self.c, None, 0))
-        table = torch.empty(max(1, self.c.num_chunks) * 32, dtype=torch.uint8)
-        _check(_lib.ss_tensor_list_plan(tensors, n, self.c, table.data_ptr(), table.numel()))
-        self._chunks = table.to(self.device)
-        self.c.chunks = self._chunks.data_ptr()
         self.state_elems = int(self.c.state_elems)
-        starts, at = [], 0
-        for p in self.params:
-            starts.append(at)
-            at += -(-p.numel() // MOMENT_BLOCK) * MOMENT_BLOCK
+        starts, start = [], 0
+        for k in numels:
+            starts.append(start)
+            start += -(-k // MOMENT_BLOCK) * MOMENT_BLOCK
         self.starts = starts
-        self._pptr = _ptr_table(self.params, self.device)
         self.grads: Optional[List[torch.Tensor]] = None
+        grads_at = at
         if grads is not None:
-            self._check_grads(list(grads))
-            self.grads = list(grads)
-        self._gptr = _ptr_table(self.params if grads is None else self.grads, self.device)
+            grads_at = self._check_grads(grads)
+            self.grads = grads
+        # the work table and both pointer arrays in one copy (the host waits for each)
+        size = self.c.num_chunks * 32
+        table = torch.empty(size // 8 + 2 * n, dtype=torch.int64)
+        _check(_lib.ss_tensor_list_plan(tensors, n, self.c, table.data_ptr(), size))
+        table[size // 8:] = torch.tensor(at + grads_at, dtype=torch.int64)
+        self._table = table.to(self.device)
+        self._pptr = self._table[size // 8:size // 8 + n]
+        self._gptr = self._table[size // 8 + n:]
+        self.c.chunks = self._table.data_ptr()
 
     def _check_grads(self, grads) -> List[int]:
         if len(grads) != len(self.params):
             raise SlipstreamError("grads: one per tensor")
-        for g, p, d in zip(grads, self.params, self.grad_dtypes):
-            if g.dtype is not d or g.numel() != p.numel() or g.device != self.device \
+        index = self.device.index
+        for g, (d, k) in zip(grads, self._grad_facts):
+            if g.dtype is not d or g.numel() != k or g.get_device() != index \
                     or not g.is_contiguous():
                 raise SlipstreamError(
-                    f"grads: need {d}, contiguous, {p.numel()} elements on {self.device}")
+                    f"grads: need {d}, contiguous, {k} elements on {self.device}")
         return [g.data_ptr() for g in grads]
 
     def set_grads(self, grads: Sequence[torch.Tensor], stream=None) -> None:
@@ -901,7 +918,8 @@ def ss_grad_norm(tensors: TensorList, max_norm: float, clip: torch.Tensor, ws: t
     _check(_lib.ss_grad_norm(
         tensors.c, tensors._gptr.data_ptr(), max_norm, grad_scale,
         _ptr_on(clip, torch.float32, "clip", tensors.device.index),
-        _ptr_on(ws, torch.uint8, "ws", tensors.device.index), ws.numel(), _stream_ptr(stream)))
+        _ptr_on(ws, torch.uint8, "ws", tensors.device.index), ws.numel(),
+        _stream_on(stream, tensors.device.index)))
 
 
 class AdamWState:
@@ -926,8 +944,13 @@ class AdamWState:
         self.master = None
         if master:
             self.master = torch.zeros(n, device=dev)
-            torch._foreach_copy_([tensors.of(self.master, k) for k in range(len(tensors.params))],
-                                 [p.detach().reshape(-1) for p in tensors.params])
+            ends = tensors.starts[1:] + [n]
+            parts = self.master.split([
+                k for p, a, b in zip(tensors.params, tensors.starts, ends)
+                for k in (p.numel(), b - a - p.numel())])[::2]
+            with torch.no_grad():
+                torch._foreach_copy_(parts, [p if p.dim() == 1 else p.reshape(-1)
+                                             for p in tensors.params])
         self.counters = torch.zeros(COUNTER_BYTES // 8, dtype=torch.int64, device=dev)
         self.c = _CAdamWState(
             bits, 0, self.m.data_ptr(), self.v.data_ptr(),
@@ -955,7 +978,7 @@ def ss_adamw_step(tensors: TensorList, state: AdamWState, lr, beta1: float = 0.9
     _check(_lib.ss_adamw_step(
         tensors.c, tensors._pptr.data_ptr(), tensors._gptr.data_ptr(), state.c, lr, at, beta1,
         beta2, eps, weight_decay, _ptr_on(clip, torch.float32, "clip", tensors.device.index),
-        _stream_ptr(stream)))
+        _stream_on(stream, tensors.device.index)))
 
 
 def ss_adamw_moments(tensors: TensorList, state: AdamWState, m: Optional[torch.Tensor],
@@ -969,12 +992,14 @@ def ss_adamw_moments(tensors: TensorList, state: AdamWState, m: Optional[torch.T
         raise SlipstreamError("ss_adamw_moments: the state belongs to another list")
     _check(_lib.ss_adamw_moments(
         tensors.c, state.c, _ptr_on(m, torch.bfloat16, "m", tensors.device.index),
-        _ptr_on(v, torch.bfloat16, "v", tensors.device.index), _stream_ptr(stream)))
+        _ptr_on(v, torch.bfloat16, "v", tensors.device.index),
+        _stream_on(stream, tensors.device.index)))
 
 
 def _matrix(who: str, name: str, t: torch.Tensor, like: torch.Tensor, shape):
     """Address and row stride of a matrix whose rows are contiguous; of like's type and device."""
-    if t.dtype is not like.dtype or t.shape != shape or t.get_device() != like.get_device():
+    if t is not like and (t.dtype is not like.dtype or t.shape != shape
+                          or t.get_device() != like.get_device()):
         raise SlipstreamError(f"{who}: {name}: matrices need one shape, type and device")
     dim = shape[1]
     if t.is_contiguous():
@@ -1029,7 +1054,7 @@ def ss_layernorm_rows_forward(x: torch.Tensor, n_valid: Optional[torch.Tensor],
     yp, ys = _matrix(who, "y", y, x, shape)
     _check(_lib.ss_layernorm_rows_forward(
         dt, wt, shape[0], shape[1], xp, xs, _ptr_on(n_valid, torch.int32, "n_valid", device), gp, bp,
-        eps, yp, ys, mp, rp, _stream_ptr(stream)))
+        eps, yp, ys, mp, rp, _stream_on(stream, device)))
 
 
 def ss_layernorm_rows_workspace_bytes(rows: int, dim: int) -> int:
@@ -1051,7 +1076,7 @@ def ss_layernorm_rows_backward(dy: torch.Tensor, x: torch.Tensor,
         dt, wt, shape[0], shape[1], dyp, dys, xp, xs,
         _ptr_on(n_valid, torch.int32, "n_valid", device), gp, mp, rp, dxp, dxs, dgp, dbp,
         _ptr_on(ws, torch.uint8, "ws", device), 0 if ws is None else ws.numel(),
-        _stream_ptr(stream)))
+        _stream_on(stream, device)))
 
 
 def stream_handle(stream=None) -> C.c_void_p:

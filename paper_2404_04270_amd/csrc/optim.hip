@@ -514,8 +514,8 @@ __device__ __forceinline__ int field_of(uint32_t bits, int least)
 
 // stepped() with the hardware's root and reciprocal, each within a step of fp32 of its value: a
 // packed step has so little to read that the exact ones show (2^28 bf16 elements 568 instead of 493
-// us).  The root takes v below 2^-126 for 0: against eps >= 1e-12 that
-// is nothing, smaller ones go the exact way.
+// us).  The root takes v below 2^-126 for 0: against eps >= 1e-12 that is nothing, smaller ones go the
+// exact way.
 constexpr double kLeastFastEps = 1e-12;
 
 __device__ __forceinline__ float stepped_fast(float p, float m, float v, const Betas &k,
