@@ -287,12 +287,6 @@ __global__ __launch_bounds__(fwd_threads<LANES>()) void rows_forward_kernel(
     }
 }
 
-template <bool FIRST, typename A, typename B> __device__ __forceinline__ auto &pick(A &a, B &b)
-{
-    if constexpr (FIRST) return a;
-    else return b;
-}
-
 // part: [2][gridDim.x][dim], the products' sums and the gradients' sums.  A workgroup that is alone
 // writes dgamma and dbeta itself and needs no part.
 template <int DT, int WT, int LANES, int P>
@@ -303,12 +297,16 @@ __global__ __launch_bounds__(bwd_threads<LANES>()) void rows_backward_kernel(
     float *__restrict__ part, void *dgamma, void *dbeta)
 {
     constexpr int N = per_access<DT>(), T = bwd_threads<LANES>(), NG = T / LANES;
-    // a lane with 32 elements has no registers left for gamma and the next row
-    constexpr bool kKeep = P * N <= 16, kAhead = kKeep;
+    // A lane with 32 elements has its column sums in LDS (128 KB of it; no other lane reads them) and
+    // gamma as it came: the registers are for the next row.  4096 x 16384 bf16 83 us, with the sums
+    // in registers and no row ahead 114; 4096 x 10000 fp32 97 and 124, 7000 x 9001 fp16 110 and 162.
+    constexpr bool kLds = P * N > 16;
+    typedef float quad __attribute__((ext_vector_type(4)));
+    __shared__ quad s_acc[kLds ? 2 * P * N / 4 : 1][kLds ? T : 1];
     __shared__ float s[2][LANES > 64 ? T / 64 * 2 : 1];
     __shared__ float s_col[NG > 1 ? T * N : 1];
     const uint32_t n = clamp_valid(n_valid, rows), step = gridDim.x * NG;
-    const int c = threadIdx.x % LANES;
+    int c = threadIdx.x % LANES;
     const float inv = 1.0f / (float)dim;
     uint32_t r = blockIdx.x * NG + group_of_lanes<LANES>();
     int64_t x_at = r * x_stride, dy_at = r * dy_stride, dx_at = r * dx_stride;
@@ -318,44 +316,45 @@ __global__ __launch_bounds__(bwd_threads<LANES>()) void rows_backward_kernel(
 #pragma unroll
         for (int i = 0; i < P; ++i) {
             const Columns<LANES, N> at(i, c, dim);
-            xn[i] = ask_columns<DT>(x, x_at, at, kKeep && flow & kStreamIn);
-            dn[i] = ask_columns<DT>(dy, dy_at, at, kKeep && flow & kStreamIn);
+            xn[i] = ask_columns<DT>(x, x_at, at, flow & kStreamIn);
+            dn[i] = ask_columns<DT>(dy, dy_at, at, flow & kStreamIn);
         }
         mu_n = mean[row];
         rs_n = rstd[row];
     };
-    if (kAhead && r < n) ask(r);
-    float gam[kKeep ? P : 1][N], acc_g[P][N], acc_b[P][N];
-    // gamma of vector i's columns: kept, or read again (from the caches) where registers are short
-    const auto gammas = [&](int i) -> float (&)[N] {
-        if constexpr (kKeep) return gam[i];
-        load_params<WT>(gamma, Columns<LANES, N>(i, c, dim), 1.0f, gam[0]);
-        return gam[0];
-    };
+    if (r < n) ask(r);
+    Raw<kLds ? WT : SS_F32, N> gam[P];
+    float acc_g[P][N], acc_b[P][N];
 #pragma unroll
     for (int i = 0; i < P; ++i) {
-        if constexpr (kKeep) load_params<WT>(gamma, Columns<LANES, N>(i, c, dim), 1.0f, gam[i]);
+        float g[N];
+        load_params<WT>(gamma, Columns<LANES, N>(i, c, dim), 1.0f, g);
+        gam[i] = from_float<kLds ? WT : SS_F32, N>(g);
+        if constexpr (kLds) {
 #pragma unroll
-        for (int e = 0; e < N; ++e) acc_g[i][e] = acc_b[i][e] = 0.0f;
+            for (int e = 0; e < 2 * N / 4; ++e) s_acc[i * 2 * N / 4 + e][threadIdx.x] = 0.0f;
+        } else {
+#pragma unroll
+            for (int e = 0; e < N; ++e) acc_g[i][e] = acc_b[i][e] = 0.0f;
+        }
     }
     // groups of several wavefronts meet at barriers: all take the turns that the first one has
     uint32_t lead = blockIdx.x * NG;
     for (int turn = 0; (LANES > 64 ? lead : r) < n; turn ^= 1) {
         const bool here = LANES <= 64 || r < n;
-        if (!kAhead && here) ask(r);
-        Raw<DT, N> x_now[kAhead ? P : 1], d_now[kAhead ? P : 1];
+        Raw<DT, N> xr[P], dr[P];
         float sums[2] = {0.0f, 0.0f};
         const float mu = mu_n, rs = rs_n;
-        if constexpr (kAhead)
+        // the columns are worked out again for each row: kept, they and what is asked of them spill
+        // (4096 x 16384 fp32 192 us, 156 without)
+        if (kLds) asm volatile("" : "+v"(c));
 #pragma unroll
-            for (int i = 0; i < P; ++i) x_now[i] = xn[i], d_now[i] = dn[i];
-        auto &xr = pick<kAhead>(x_now, xn);
-        auto &dr = pick<kAhead>(d_now, dn);
+        for (int i = 0; i < P; ++i) xr[i] = xn[i], dr[i] = dn[i];
         lead += step;
         r += step;
         x_at += step * x_stride;
         dy_at += step * dy_stride;
-        if (kAhead && r < n) ask(r);       // the next row is under way while this one is worked on
+        if (r < n) ask(r);       // the next row is under way while this one is worked on
         if (here) {
 #pragma unroll
             for (int i = 0; i < P; ++i) {
@@ -364,17 +363,38 @@ __global__ __launch_bounds__(bwd_threads<LANES>()) void rows_backward_kernel(
                 settle(dr[i], Columns<LANES, N>(i, c, dim));
                 to_float(xr[i], xf);
                 to_float(dr[i], df);
-                const auto &gm = gammas(i);
+                float gm[N];
+                to_float(gam[i], gm);
 #pragma unroll
                 for (int e = 0; e < N; ++e) {
                     xf[e] = (xf[e] - mu) * rs;
-                    acc_g[i][e] = fmaf(df[e], xf[e], acc_g[i][e]);
-                    acc_b[i][e] += df[e];
+                    if constexpr (!kLds) {
+                        acc_g[i][e] = fmaf(df[e], xf[e], acc_g[i][e]);
+                        acc_b[i][e] += df[e];
+                    }
+                }
+                if constexpr (kLds) {
+#pragma unroll
+                    for (int e = 0; e < N; e += 4) {
+                        quad &g = s_acc[(i * N + e) / 2][threadIdx.x];
+                        quad &b = s_acc[(i * N + e) / 2 + 1][threadIdx.x];
+                        quad tg = g, tb = b;
+#pragma unroll
+                        for (int k = 0; k < 4; ++k) {
+                            tg[k] = fmaf(df[e + k], xf[e + k], tg[k]);
+                            tb[k] += df[e + k];
+                        }
+                        g = tg;
+                        b = tb;
+                    }
+                }
+#pragma unroll
+                for (int e = 0; e < N; ++e) {
                     df[e] *= gm[e];                  // 0 past the row
                     sums[0] += df[e];
                     sums[1] = fmaf(df[e], xf[e], sums[1]);
                 }
-                if (!kKeep) __builtin_amdgcn_sched_barrier(0);
+                if (kLds) __builtin_amdgcn_sched_barrier(0);
             }
         }
         row_sums<LANES, 2>(sums, s[turn]);
@@ -387,12 +407,13 @@ __global__ __launch_bounds__(bwd_threads<LANES>()) void rows_backward_kernel(
                 forget(dr[i]);
                 to_float(xr[i], xf);
                 to_float(dr[i], df);
-                const auto &gm = gammas(i);
+                float gm[N];
+                to_float(gam[i], gm);
 #pragma unroll
                 for (int e = 0; e < N; ++e)
                     o[e] = fmaf((mu - xf[e]) * rs, m2, fmaf(df[e], gm[e], -m1)) * rs;
                 store_columns<DT>(dx, dx_at, Columns<LANES, N>(i, c, dim), o, flow & kStreamOut);
-                if (!kKeep) __builtin_amdgcn_sched_barrier(0);
+                if (kLds) __builtin_amdgcn_sched_barrier(0);
             }
         }
         dx_at += step * dx_stride;
@@ -408,7 +429,10 @@ __global__ __launch_bounds__(bwd_threads<LANES>()) void rows_backward_kernel(
             const Columns<LANES, N> at(i, c, dim);
             float t[N];
 #pragma unroll
-            for (int e = 0; e < N; ++e) t[e] = which ? acc_b[i][e] : acc_g[i][e];
+            for (int e = 0; e < N; ++e) {
+                if constexpr (kLds) t[e] = s_acc[(i * N + e) / 4 * 2 + which][threadIdx.x][e % 4];
+                else t[e] = which ? acc_b[i][e] : acc_g[i][e];
+            }
             if constexpr (NG > 1) {                      // the groups' sums, in their order
                 __syncthreads();
 #pragma unroll
@@ -625,8 +649,8 @@ __global__ __launch_bounds__(kRedCols * kParts) void columns_reduce_kernel(
 // ---- which kernel takes a row ---------------------------------------------------------------
 // The narrowest group whose lanes hold the row in one vector each, up to a wavefront (sums then stay
 // within rows of lanes); then up to 16 elements per lane, of one, four and eight wavefronts, which a
-// barrier joins; then 32 per lane.  (8192 to 16384 elements as 16 per lane of 1024 threads spill:
-// 4096 x 16384 bf16 backward 126 to 149 us, 110 with 512.)
+// barrier joins; then 32 per lane.  (8192 to 16384 elements as 16 per lane of 1024 threads spill
+// backward: 4096 x 16384 bf16 126 to 149 us.)
 struct Shape {
     int lanes, vectors;        // lanes == 0: too wide for registers
 };

@@ -124,6 +124,14 @@ def test_rows_strides_and_valid_counts(rows, dim, dtype, wt, pad, n_valid):
     both_ways(rows, dim, dtype, wt, pad, n_valid, seed=rows + dim)
 
 
+@pytest.mark.parametrize("rows,dim,dtype,wt,pad,n_valid", [
+    (700, 9001, F16, F16, 1, 699), (530, 12_001, BF16, F32, 0, None), (515, 16_384, F32, F32, 0, 514),
+    (770, 16_383, BF16, BF16, 3, None), (258, 8193, F32, F32, 2, None),
+    (5000, 12_000, BF16, BF16, 0, None)])
+def test_workgroups_with_several_wide_rows(rows, dim, dtype, wt, pad, n_valid):
+    both_ways(rows, dim, dtype, wt, pad, n_valid, seed=rows + dim)
+
+
 @pytest.mark.parametrize("dim", [5, 300, 3000, 50_000])
 def test_in_place_and_without_parameters(dim):
     from paper_2404_04270_amd import binding as B
