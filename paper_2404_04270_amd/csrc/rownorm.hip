@@ -287,6 +287,13 @@ __global__ __launch_bounds__(fwd_threads<LANES>()) void rows_forward_kernel(
     }
 }
 
+// Whether vector i lies past the row for all lanes of this wavefront.
+template <int LANES, int N> __device__ __forceinline__ bool past(int i, int dim)
+{
+    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x % LANES / 64);
+    return (i * LANES + wave * 64) * N >= dim;
+}
+
 // part: [2][gridDim.x][dim], the products' sums and the gradients' sums.  A workgroup that is alone
 // writes dgamma and dbeta itself and needs no part.
 template <int DT, int WT, int LANES, int P>
@@ -298,8 +305,10 @@ __global__ __launch_bounds__(bwd_threads<LANES>()) void rows_backward_kernel(
 {
     constexpr int N = per_access<DT>(), T = bwd_threads<LANES>(), NG = T / LANES;
     // A lane with 32 elements has its column sums in LDS (128 KB of it; no other lane reads them) and
-    // gamma as it came: the registers are for the next row.  4096 x 16384 bf16 83 us, with the sums
-    // in registers and no row ahead 114; 4096 x 10000 fp32 97 and 124, 7000 x 9001 fp16 110 and 162.
+    // gamma as it came: the registers are for the next row.  4096 x 16384 bf16 84 us, with the sums
+    // in registers and no row ahead 114; 4096 x 10000 fp32 97 and 124, 7000 x 9000 fp16 91 and 150.
+    // Its wavefronts leave out the vectors past the row (7000 x 9000 fp16 102 us without; where a row
+    // of fewer elements has several vectors per lane it costs as much as it saves).
     constexpr bool kLds = P * N > 16;
     typedef float quad __attribute__((ext_vector_type(4)));
     __shared__ quad s_acc[kLds ? 2 * P * N / 4 : 1][kLds ? T : 1];
@@ -358,6 +367,7 @@ __global__ __launch_bounds__(bwd_threads<LANES>()) void rows_backward_kernel(
         if (here) {
 #pragma unroll
             for (int i = 0; i < P; ++i) {
+                if (kLds && past<LANES, N>(i, dim)) break;
                 float xf[N], df[N];
                 settle(xr[i], Columns<LANES, N>(i, c, dim));
                 settle(dr[i], Columns<LANES, N>(i, c, dim));
@@ -402,6 +412,7 @@ __global__ __launch_bounds__(bwd_threads<LANES>()) void rows_backward_kernel(
         if (here) {
 #pragma unroll
             for (int i = 0; i < P; ++i) {
+                if (kLds && past<LANES, N>(i, dim)) break;
                 float xf[N], df[N], o[N];
                 forget(xr[i]);
                 forget(dr[i]);
