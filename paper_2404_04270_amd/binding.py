@@ -154,6 +154,12 @@ def _check(rc: int):
             f"[{rc}] " + _lib.ss_last_error().decode("utf-8", "replace"))
 
 
+def _beyond(*sizes: int) -> bool:
+    """Whether a size is negative or does not fit an int32 argument: ctypes would pass its lower 32
+    bits on without a word, and a smaller problem would be worked on."""
+    return any(n >> 31 for n in sizes)
+
+
 def ss_last_error() -> str:
     return _lib.ss_last_error().decode("utf-8", "replace")
 
@@ -1021,6 +1027,8 @@ def _rows_args(who: str, x: torch.Tensor, params, mean: torch.Tensor, rstd: torc
     if dtype not in DTYPES:
         raise SlipstreamError(f"{who}: {dtype} is not one of fp32, bf16, fp16")
     rows, dim = shape
+    if (rows | dim) >> 31:               # as _beyond, in line
+        raise SlipstreamError(f"{who}: {rows} x {dim}: rows or columns beyond 32 bits")
     wt, at = None, []
     for p in params:
         if p is None:
@@ -1058,6 +1066,9 @@ def ss_layernorm_rows_forward(x: torch.Tensor, n_valid: Optional[torch.Tensor],
 
 
 def ss_layernorm_rows_workspace_bytes(rows: int, dim: int) -> int:
+    """0 for sizes that the calls do not take."""
+    if _beyond(rows, dim):
+        return 0
     return int(_lib.ss_layernorm_rows_workspace_bytes(rows, dim))
 
 
