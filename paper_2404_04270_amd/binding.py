@@ -155,9 +155,14 @@ def _check(rc: int):
 
 
 def _beyond(*sizes: int) -> bool:
-    """Whether a size is negative or does not fit an int32 argument: ctypes would pass its lower 32
-    bits on without a word, and a smaller problem would be worked on."""
-    return any(n >> 31 for n in sizes)
+    """Whether a size does not fit an int32 argument: ctypes would pass its lower 32 bits on without a
+    word, and a smaller problem would be worked on."""
+    return any((n + (1 << 31)) >> 32 for n in sizes)
+
+
+def _fits(who: str, *sizes: int) -> None:
+    if _beyond(*sizes):
+        raise SlipstreamError(f"{who}: a size of {' x '.join(map(str, sizes))} is beyond 32 bits")
 
 
 def ss_last_error() -> str:
@@ -177,6 +182,7 @@ def ss_check_indices(num_tables: int, rows: int, idx: torch.Tensor,
     table << 32 | position of the first one, or -1)."""
     if idx.dim() != 3 or idx.shape[0] != num_tables:
         raise SlipstreamError("ss_check_indices: idx must be [T, B, L]")
+    _fits("ss_check_indices", *idx.shape)
     if report.numel() < 2:
         raise SlipstreamError("ss_check_indices: report needs two words")
     _check(_lib.ss_check_indices(
@@ -271,6 +277,7 @@ class Tables:
         w0 = self.weights[0]
         self.device = w0.device
         self.rows, self.dim = int(w0.shape[0]), int(w0.shape[1])
+        _fits("weights: dim", self.dim)
         for w in self.weights:
             _dev_ptr(w, torch.float32, "weights")
             if tuple(w.shape) != (self.rows, self.dim):
@@ -319,11 +326,17 @@ class Tables:
 
 
 def ss_filter_batch_workspace_bytes(T: int, B: int, L: int) -> int:
+    """0 for sizes that the calls do not take."""
+    if _beyond(T, B, L):
+        return 0
     return int(_lib.ss_filter_batch_workspace_bytes(
         C.c_int32(T), C.c_int32(B), C.c_int32(L)))
 
 
 def ss_backward_workspace_bytes(T: int, Bcap: int, L: int, dim: int) -> int:
+    """0 for sizes that the calls do not take."""
+    if _beyond(T, Bcap, L, dim):
+        return 0
     return int(_lib.ss_backward_workspace_bytes(
         C.c_int32(T), C.c_int32(Bcap), C.c_int32(L), C.c_int32(dim)))
 
@@ -331,7 +344,10 @@ def ss_backward_workspace_bytes(T: int, Bcap: int, L: int, dim: int) -> int:
 def _idx_shape(tables: Tables, idx: torch.Tensor):
     if idx.dim() != 3 or idx.shape[0] != tables.num_tables:
         raise SlipstreamError("idx: need int32 [T, B, L]")
-    return int(idx.shape[1]), int(idx.shape[2])
+    B, L = int(idx.shape[1]), int(idx.shape[2])
+    if (B | L) >> 31:                    # (in line: a tenth of the time of a call)
+        _fits("idx", B, L)
+    return B, L
 
 
 def ss_filter_batch(tables: Tables, idx: torch.Tensor, alpha: int,
@@ -448,6 +464,8 @@ def ss_embbag_backward_apply(tables: Tables, Bcap: int, L: int, grad: torch.Tens
                              lr: float, ws: torch.Tensor, stream=None) -> None:
     if grad.numel() < tables.num_tables * Bcap * tables.dim:
         raise SlipstreamError("ss_embbag_backward_apply: grad is too small")
+    if (Bcap | L) >> 31:
+        _fits("ss_embbag_backward_apply", Bcap, L)
     _check(_lib.ss_embbag_backward_apply(
         tables.c, Bcap, L,
         _ptr(grad, torch.float32, "grad"), lr,
@@ -467,6 +485,7 @@ class HotState:
         dev = tables.device
         self.hot_ids = list(hot_ids)
         self.H = int(self.hot_ids[0].numel())
+        _fits("hot_ids", self.H)
         T = tables.num_tables
         for h in self.hot_ids:
             _dev_ptr(h, torch.int32, "hot_ids")
@@ -512,6 +531,7 @@ def ss_sample_drop(hot: HotState, sidx: torch.Tensor, alpha: int,
         raise SlipstreamError("ss_sample_drop: HotState was built without diagnostics")
     if sidx.dim() != 3 or sidx.shape[0] != len(hot.hot_ids):
         raise SlipstreamError("ss_sample_drop: sidx must be [T, S, L]")
+    _fits("ss_sample_drop", *sidx.shape)
     thr = (C.c_float * len(thresholds))(*[float(x) for x in thresholds])
     if counts.numel() < len(thresholds):
         raise SlipstreamError("ss_sample_drop: counts is shorter than thresholds")
@@ -547,6 +567,7 @@ def ss_sample_levels(hot: HotState, sidx: torch.Tensor, levels: torch.Tensor,
         raise SlipstreamError("ss_sample_levels: HotState was built without diagnostics")
     if sidx.dim() != 3 or sidx.shape[0] != len(hot.hot_ids):
         raise SlipstreamError("ss_sample_levels: sidx must be [T, S, L]")
+    _fits("ss_sample_levels", *sidx.shape)
     if levels.numel() != sidx.shape[1]:
         # (ss_level_counts counts all the levels it is given)
         raise SlipstreamError("ss_sample_levels: levels needs one entry per sampled input")
@@ -562,6 +583,7 @@ def ss_level_counts(levels: torch.Tensor, thresholds: Sequence[float], counts: t
     thr = array("f", thresholds)           # (a third of the time of a ctypes array of 34)
     if counts.numel() < len(thresholds):
         raise SlipstreamError("ss_level_counts: counts is shorter than thresholds")
+    _fits("ss_level_counts", levels.numel())
     _check(_lib.ss_level_counts(
         _ptr(levels, torch.float32, "levels"), levels.numel(), thr.buffer_info()[0], len(thr),
         _ptr(counts, torch.int32, "counts"), _stream_ptr(stream)))
@@ -633,6 +655,7 @@ def ss_count_accesses(counters: AccessCounters, idx: torch.Tensor,
                       n_valid: Optional[torch.Tensor] = None, stream=None) -> None:
     if idx.dim() != 3 or idx.shape[0] != len(counters.counts):
         raise SlipstreamError("ss_count_accesses: idx must be [T, B, L]")
+    _fits("ss_count_accesses", *idx.shape)
     _check(_lib.ss_count_accesses(
         len(counters.counts), counters.rows,
         _ptr(idx, torch.int32, "idx"), idx.shape[1],
@@ -653,6 +676,7 @@ def ss_select_hot_ratio(counters: AccessCounters, lam: float, total: int,
     dev = counters.device
     T = len(counters.counts)
     cap = 0 if hot_ids is None else int(hot_ids[0].numel())
+    _fits("ss_select_hot_ratio", cap)
     if hot_ids is not None and any(h.numel() != cap for h in hot_ids):
         raise SlipstreamError("ss_select_hot_ratio: hot_ids need one length")
     if hot_bits is not None and any(b.numel() < Tables.bitmap_words(counters.rows)
@@ -677,6 +701,7 @@ def ss_select_hot_top(counters: AccessCounters, H: int,
                       stream=None) -> None:
     dev = counters.device
     T = len(counters.counts)
+    _fits("ss_select_hot_top", H)
     if hot_ids is not None and any(h.numel() < H for h in hot_ids):
         raise SlipstreamError("ss_select_hot_top: hot_ids shorter than H")
     if hot_bits is not None and any(b.numel() < Tables.bitmap_words(counters.rows)
@@ -694,7 +719,10 @@ def ss_select_hot_top(counters: AccessCounters, H: int,
 def _ln_shape(x: torch.Tensor):
     if x.dim() != 3:
         raise SlipstreamError("layernorm: need fp32 [T, Bcap, D]")
-    return int(x.shape[0]), int(x.shape[1]), int(x.shape[2])
+    T, Bcap, D = int(x.shape[0]), int(x.shape[1]), int(x.shape[2])
+    if (T | Bcap | D) >> 31:
+        _fits("layernorm", T, Bcap, D)
+    return T, Bcap, D
 
 
 def ss_layernorm_forward(x: torch.Tensor, n_valid: Optional[torch.Tensor],
@@ -716,6 +744,9 @@ def ss_layernorm_forward(x: torch.Tensor, n_valid: Optional[torch.Tensor],
 
 
 def ss_layernorm_backward_workspace_bytes(T: int, dim: int, Bcap: int) -> int:
+    """0 for sizes that the calls do not take."""
+    if _beyond(T, dim, Bcap):
+        return 0
     return int(_lib.ss_layernorm_backward_workspace_bytes(
         C.c_int32(T), C.c_int32(dim), C.c_int32(Bcap)))
 
@@ -1027,8 +1058,8 @@ def _rows_args(who: str, x: torch.Tensor, params, mean: torch.Tensor, rstd: torc
     if dtype not in DTYPES:
         raise SlipstreamError(f"{who}: {dtype} is not one of fp32, bf16, fp16")
     rows, dim = shape
-    if (rows | dim) >> 31:               # as _beyond, in line
-        raise SlipstreamError(f"{who}: {rows} x {dim}: rows or columns beyond 32 bits")
+    if (rows | dim) >> 31:
+        _fits(who, rows, dim)
     wt, at = None, []
     for p in params:
         if p is None:
@@ -1250,6 +1281,7 @@ def ss_step_plan_for(T: int, B: int, L: int, every: int = 0, index_streams: int 
                      issue_threads: int = -1, host_wait_us: int = -1, dim: int = 0) -> StepPlan:
     """The plan for a shape; 0 / 0 / -1 / -1 leave the choice to the library (dim = 0:
     the row length is not known)."""
+    _fits("ss_step_plan_for", T, B, L)
     plan = StepPlan(int(every), int(index_streams), int(issue_threads), 0, int(host_wait_us),
                     int(dim))
     _check(_lib.ss_step_plan_for(C.c_int32(T), C.c_int32(B), C.c_int32(L), C.byref(plan)))
@@ -1261,6 +1293,7 @@ def ss_step_create(tables: Tables, B: int, L: int, alpha: int, lr: float, thresh
                    stream=None) -> C.c_void_p:
     """sets: plan.num_sets objects with skip_mask, kept_ids, n_kept, idx_c, ws_filter and
     ws_backward tensors.  Returns the handle of the native step."""
+    _fits("ss_step_create", B, L)
     if len(sets) != plan.num_sets:
         raise SlipstreamError("ss_step_create: need plan.num_sets buffer sets")
     if pooled.numel() < tables.num_tables * B * tables.dim:
