@@ -5,9 +5,9 @@ pass and the next batch, beside the tables' own update (ss_embbag_backward_updat
     opt.set_grads([p.grad for p in params])
     opt.step()
 
-This class only owns buffers and issues the library calls in order; nothing here synchronises with
-the host.  step() can be captured in a graph: steps are counted on the device, and with
-lr a device tensor the schedule is, too.
+This class only owns buffers and issues the library calls in order; nothing in set_grads, step and
+moments synchronises with the host.  step() can be captured in a graph: steps are counted on the
+device, and with lr a device tensor the schedule is, too.
 """
 from __future__ import annotations
 
@@ -54,17 +54,40 @@ class AdamW:
         """The gradient tensors that steps read from now on."""
         self.list.set_grads(grads, stream)
 
-    def set_step(self, steps: int) -> None:
-        """Number of steps taken so far (a restored state's)."""
-        self.state.counters[0] = steps
+    def set_step(self, steps: int, stream=None) -> None:
+        """Number of steps taken so far (a restored state's).  With a stream the count is set in order
+        on it, and under capture on the current one; otherwise the call waits for the device on
+        both sides, so that it comes behind the steps of every stream and before those that
+        follow."""
+        if steps < 0:
+            raise B.SlipstreamError(f"set_step: steps = {steps}")
+        count = self.state.counters[:1]
+        if stream is not None:
+            with torch.cuda.stream(stream):
+                count.fill_(steps)
+        elif torch.cuda.is_current_stream_capturing():
+            count.fill_(steps)
+        else:
+            torch.cuda.synchronize(self.list.device)
+            count.fill_(steps)
+            torch.cuda.synchronize(self.list.device)
 
-    def steps(self) -> int:
-        """Steps taken so far; waits for the device."""
-        return int(self.state.counters[0])
+    def steps(self, stream=None) -> int:
+        """Steps taken so far; waits for the device (while no stream of it is under capture), with a
+        stream for that one only."""
+        return self._counter(0, stream)
 
-    def left_out(self) -> int:
-        """Steps left out because the gradients' norm was not finite; waits for the device."""
-        return int(self.state.counters[1])
+    def left_out(self, stream=None) -> int:
+        """Steps left out because the gradients' norm was not finite; waits as steps()."""
+        return self._counter(1, stream)
+
+    def _counter(self, k: int, stream) -> int:
+        # (reading a tensor waits for the current stream alone; steps may run on others)
+        if stream is None:
+            torch.cuda.synchronize(self.list.device)
+            return int(self.state.counters[k])
+        with torch.cuda.stream(stream):
+            return int(self.state.counters[k])
 
     def step(self, clip: Optional[torch.Tensor] = None, stream=None) -> None:
         """clip: fp32 [4] as ss_grad_norm writes it (one norm over several optimizers, say); without
