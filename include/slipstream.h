@@ -509,7 +509,8 @@ int32_t ss_grad_norm(const ss_tensor_list *list, const void *const *grads, doubl
  *   bits      32: m and v are float [state_elems]
  *             8: m and v are uint8 [state_elems], exps is uint8 [state_elems / SS_MOMENT_BLOCK][2];
  *             see below
- *   master    float [state_elems] or NULL; used for the tensors of 16 bits
+ *   master    float [state_elems] or NULL; used for the tensors of 16 bits (the places of the others
+ *             are neither read nor written)
  *   counters  SS_ADAMW_COUNTER_BYTES, 64-byte aligned, zeroed before the first step: int64 steps
  *             taken, int64 steps left out, and what belongs to the step in progress.  A step
  *             counts itself on the device, so that it can be captured in a graph and replayed;

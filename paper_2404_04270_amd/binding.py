@@ -963,8 +963,9 @@ class AdamWState:
     """Moments of a list's tensors in 32 or in 8 bits, fp32 copies of its 16-bit parameters if
     asked for, and the step's counters: zeros before the first step, made on the current stream.
     Arrays hold the tensors one after the other, each padded to MOMENT_BLOCK elements
-    (TensorList.of cuts one out); a checkpoint holds m, v, exps, master and counters as they are.  A
-    program that writes to 16-bit parameters between steps writes to their copies, too."""
+    (TensorList.of cuts one out); the copies' places of fp32 parameters, which have none, stay 0.  A
+    checkpoint holds m, v, exps, master and counters as they are.  A program that writes to 16-bit
+    parameters between steps writes to their copies, too."""
 
     def __init__(self, tensors: TensorList, bits: int = 32, master: bool = False):
         if bits not in (32, 8):
@@ -985,9 +986,11 @@ class AdamWState:
             parts = self.master.split([
                 k for p, a, b in zip(tensors.params, tensors.starts, ends)
                 for k in (p.numel(), b - a - p.numel())])[::2]
-            with torch.no_grad():
-                torch._foreach_copy_(parts, [p if p.dim() == 1 else p.reshape(-1)
-                                             for p in tensors.params])
+            narrow = [(c, p if p.dim() == 1 else p.reshape(-1))
+                      for c, p in zip(parts, tensors.params) if p.dtype is not torch.float32]
+            if narrow:
+                with torch.no_grad():
+                    torch._foreach_copy_(*zip(*narrow))
         self.counters = torch.zeros(COUNTER_BYTES // 8, dtype=torch.int64, device=dev)
         self.c = _CAdamWState(
             bits, 0, self.m.data_ptr(), self.v.data_ptr(),
