@@ -1028,12 +1028,18 @@ def ss_adamw_moments(tensors: TensorList, state: AdamWState, m: Optional[torch.T
     for out in (m, v):
         if out is not None and out.numel() < state.m.numel():
             raise SlipstreamError("ss_adamw_moments: an output is too small")
-    if state.m.numel() != tensors.state_elems:
+    if state.m.numel() != tensors.state_elems or state.m.device != tensors.device:
         raise SlipstreamError("ss_adamw_moments: the state belongs to another list")
     _check(_lib.ss_adamw_moments(
         tensors.c, state.c, _ptr_on(m, torch.bfloat16, "m", tensors.device.index),
         _ptr_on(v, torch.bfloat16, "v", tensors.device.index),
         _stream_on(stream, tensors.device.index)))
+
+
+def _valid_rows(who: str, n_valid: Optional[torch.Tensor], index: int):
+    if n_valid is not None and n_valid.numel() == 0:
+        raise SlipstreamError(f"{who}: n_valid needs one int32")
+    return _ptr_on(n_valid, torch.int32, "n_valid", index)
 
 
 def _matrix(who: str, name: str, t: torch.Tensor, like: torch.Tensor, shape):
@@ -1095,8 +1101,8 @@ def ss_layernorm_rows_forward(x: torch.Tensor, n_valid: Optional[torch.Tensor],
     xp, xs = _matrix(who, "x", x, x, shape)
     yp, ys = _matrix(who, "y", y, x, shape)
     _check(_lib.ss_layernorm_rows_forward(
-        dt, wt, shape[0], shape[1], xp, xs, _ptr_on(n_valid, torch.int32, "n_valid", device), gp, bp,
-        eps, yp, ys, mp, rp, _stream_on(stream, device)))
+        dt, wt, shape[0], shape[1], xp, xs, _valid_rows(who, n_valid, device), gp, bp, eps, yp, ys,
+        mp, rp, _stream_on(stream, device)))
 
 
 def ss_layernorm_rows_workspace_bytes(rows: int, dim: int) -> int:
@@ -1119,7 +1125,7 @@ def ss_layernorm_rows_backward(dy: torch.Tensor, x: torch.Tensor,
     dxp, dxs = _matrix(who, "dx", dx, x, shape)
     _check(_lib.ss_layernorm_rows_backward(
         dt, wt, shape[0], shape[1], dyp, dys, xp, xs,
-        _ptr_on(n_valid, torch.int32, "n_valid", device), gp, mp, rp, dxp, dxs, dgp, dbp,
+        _valid_rows(who, n_valid, device), gp, mp, rp, dxp, dxs, dgp, dbp,
         _ptr_on(ws, torch.uint8, "ws", device), 0 if ws is None else ws.numel(),
         _stream_on(stream, device)))
 
