@@ -26,11 +26,11 @@ constexpr int kStreamOut = 1, kStreamIn = 2;       // past the caches
 // Elements per 16-byte access.
 template <int DT> constexpr int per_access() { return DT == SS_F32 ? 4 : 8; }
 
-// Threads of a workgroup: forward few, so that several share a compute unit; backward more, since
+// Threads of a workgroup: forward few, so that several share a compute unit; backward 512, since
 // every workgroup ends in a partial row of the parameters' gradients.  (With 1024 each of them has
 // 128 registers and spills: 32768 x 4096 bf16 backward 159 us, 150 with 512.)
 template <int LANES> constexpr int fwd_threads() { return LANES > kWG ? LANES : kWG; }
-template <int LANES> constexpr int bwd_threads() { return LANES > 512 ? LANES : 512; }
+constexpr int kBwdThreads = 512;
 
 template <int CTRL> __device__ __forceinline__ float dpp(float v)
 {
@@ -297,13 +297,13 @@ template <int LANES, int N> __device__ __forceinline__ bool past(int i, int dim)
 // part: [2][gridDim.x][dim], the products' sums and the gradients' sums.  A workgroup that is alone
 // writes dgamma and dbeta itself and needs no part.
 template <int DT, int WT, int LANES, int P>
-__global__ __launch_bounds__(bwd_threads<LANES>()) void rows_backward_kernel(
+__global__ __launch_bounds__(kBwdThreads) void rows_backward_kernel(
     const void *dy, int64_t dy_stride, const void *x, int64_t x_stride, int rows,
     const int32_t *__restrict__ n_valid, const void *gamma, const float *__restrict__ mean,
     const float *__restrict__ rstd, void *dx, int64_t dx_stride, int dim, int flow,
     float *__restrict__ part, void *dgamma, void *dbeta)
 {
-    constexpr int N = per_access<DT>(), T = bwd_threads<LANES>(), NG = T / LANES;
+    constexpr int N = per_access<DT>(), T = kBwdThreads, NG = T / LANES;
     // A lane with 32 elements has its column sums in LDS (128 KB of it; no other lane reads them) and
     // gamma as it came: the registers are for the next row.  4096 x 16384 bf16 84 us, with the sums
     // in registers and no row ahead 114; 4096 x 10000 fp32 97 and 124, 7000 x 9000 fp16 91 and 150.
@@ -510,19 +510,17 @@ __global__ __launch_bounds__(kWideThreads) void wide_forward_kernel(
     for (int64_t r = blockIdx.x; r < n; r += gridDim.x) {
         float sum = 0.0f, q = 0.0f;
         for (int col = threadIdx.x * N; col < dim; col += T * N) {
-            Raw<DT, N> raw[1];
+            const Raw<DT, N> raw = load_some<DT, N>(x, r * x_stride, col, dim);
             float f[N];
-            raw[0] = load_some<DT, N>(x, r * x_stride, col, dim);
-            to_float(raw[0], f);
+            to_float(raw, f);
 #pragma unroll
             for (int k = 0; k < N; ++k) sum += f[k];
         }
         const float mu = row_sum<T>(sum, s[0]) * inv;
         for (int col = threadIdx.x * N; col < dim; col += T * N) {
-            Raw<DT, N> raw[1];
+            const Raw<DT, N> raw = load_some<DT, N>(x, r * x_stride, col, dim);
             float f[N];
-            raw[0] = load_some<DT, N>(x, r * x_stride, col, dim);
-            to_float(raw[0], f);
+            to_float(raw, f);
 #pragma unroll
             for (int k = 0; k < N; ++k) {
                 const float d = col + k < dim ? f[k] - mu : 0.0f;
@@ -531,14 +529,13 @@ __global__ __launch_bounds__(kWideThreads) void wide_forward_kernel(
         }
         const float rs = 1.0f / sqrtf(fmaf(row_sum<T>(q, s[1]), inv, eps));
         for (int col = threadIdx.x * N; col < dim; col += T * N) {
-            Raw<DT, N> raw[1];
-            float f[N], gam[1][N], bet[1][N];
-            raw[0] = load_some<DT, N>(x, r * x_stride, col, dim);
-            some_params<WT, N>(gamma, col, dim, 1.0f, gam[0]);
-            some_params<WT, N>(beta, col, dim, 0.0f, bet[0]);
-            to_float(raw[0], f);
+            const Raw<DT, N> raw = load_some<DT, N>(x, r * x_stride, col, dim);
+            float f[N], gam[N], bet[N];
+            some_params<WT, N>(gamma, col, dim, 1.0f, gam);
+            some_params<WT, N>(beta, col, dim, 0.0f, bet);
+            to_float(raw, f);
 #pragma unroll
-            for (int k = 0; k < N; ++k) f[k] = fmaf((f[k] - mu) * rs, gam[0][k], bet[0][k]);
+            for (int k = 0; k < N; ++k) f[k] = fmaf((f[k] - mu) * rs, gam[k], bet[k]);
             store_some<DT, N>(y, r * y_stride, col, dim, f);
         }
         if (threadIdx.x == 0) {
@@ -564,19 +561,18 @@ __global__ __launch_bounds__(kWideThreads) void wide_backward_kernel(
         float s1 = 0.0f, s2 = 0.0f, m1 = 0.0f, m2 = 0.0f;
         for (int pass = 0; pass < 2; ++pass) {
             for (int col = threadIdx.x * N; col < dim; col += T * N) {
-                Raw<DT, N> xr[1], dr[1];
-                float xf[N], df[N], gam[1][N];
-                xr[0] = load_some<DT, N>(x, r * x_stride, col, dim);
-                dr[0] = load_some<DT, N>(dy, r * dy_stride, col, dim);
-                some_params<WT, N>(gamma, col, dim, 1.0f, gam[0]);
-                to_float(xr[0], xf);
-                to_float(dr[0], df);
+                const Raw<DT, N> xr = load_some<DT, N>(x, r * x_stride, col, dim);
+                const Raw<DT, N> dr = load_some<DT, N>(dy, r * dy_stride, col, dim);
+                float xf[N], df[N], gam[N];
+                some_params<WT, N>(gamma, col, dim, 1.0f, gam);
+                to_float(xr, xf);
+                to_float(dr, df);
 #pragma unroll
                 for (int k = 0; k < N; ++k) {
-                    const float xh = (xf[k] - mu) * rs, gd = gam[0][k] * df[k];
+                    const float xh = (xf[k] - mu) * rs, gd = gam[k] * df[k];
                     s1 += gd;
                     s2 = fmaf(gd, xh, s2);
-                    df[k] = fmaf(-xh, m2, fmaf(gam[0][k], df[k], -m1)) * rs;
+                    df[k] = fmaf(-xh, m2, fmaf(gam[k], df[k], -m1)) * rs;
                 }
                 if (pass) store_some<DT, N>(dx, r * dx_stride, col, dim, df);
             }
@@ -604,13 +600,12 @@ __global__ __launch_bounds__(kWG) void wide_columns_kernel(
     for (int k = 0; k < N; ++k) acc_g[k] = acc_b[k] = 0.0f;
 #pragma unroll 2
     for (int64_t r = blockIdx.y; r < n; r += gridDim.y) {
-        Raw<DT, N> xr[1], dr[1];
+        const Raw<DT, N> xr = load_some<DT, N>(x, r * x_stride, (int)col, dim);
+        const Raw<DT, N> dr = load_some<DT, N>(dy, r * dy_stride, (int)col, dim);
         float xf[N], df[N];
-        xr[0] = load_some<DT, N>(x, r * x_stride, (int)col, dim);
-        dr[0] = load_some<DT, N>(dy, r * dy_stride, (int)col, dim);
         const float mu = mean[r], rs = rstd[r];
-        to_float(xr[0], xf);
-        to_float(dr[0], df);
+        to_float(xr, xf);
+        to_float(dr, df);
 #pragma unroll
         for (int k = 0; k < N; ++k) {
             acc_g[k] = fmaf(df[k], (xf[k] - mu) * rs, acc_g[k]);
@@ -862,7 +857,7 @@ int32_t ss_layernorm_rows_backward(int32_t dtype, int32_t param_dtype, int32_t r
     if (rows > 0) {
         const int most = most_parts(rows, dim);
 #define SS_ROWS_BWD                                                                           \
-    const int threads = bwd_threads<LANES>();                                                 \
+    const int threads = kBwdThreads;                                                          \
     const int64_t groups = threads / LANES, need = (rows + groups - 1) / groups;              \
     n_part = (int)(need < most ? need : most);                                                \
     const int wgs = P > 1 ? kBackwardWgs : 2 * kBackwardWgs;                                  \
