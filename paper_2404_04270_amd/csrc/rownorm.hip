@@ -726,11 +726,19 @@ constexpr int kWideWgs = 1024;
 // Workgroups of a backward launch: one per compute unit.  Two where a lane has one vector of a row,
 // and so half as much under way: 16384 x 2048 bf16 44 us with two and 55 with one, 300000 x 100
 // fp32 71 and 81.  Elsewhere the second adds partial rows and nothing else: 32768 x 4096 bf16 157 and
-// 150, 2048 x 4096 19.6 and 17.2, 16384 x 1024 29.3 and 24.4.
+// 150, 2048 x 4096 19.6 and 17.2, 16384 x 1024 29.3 and 24.4.  The same without column sums: with up to
+// 1024 workgroups 10007 x 1001 fp16 takes 17.1 instead of 12.8 us, 16384 x 1024 bf16 20.4 and 17.2,
+// 300000 x 100 fp32 71 and 65, 7000 x 9001 fp16 96 and 91, 4096 x 16384 bf16 80 and 71 (32768 x 4096
+// bf16 132 and 136, 8192 x 8192 67 and 69).
 constexpr int kBackwardWgs = 256;
-// Up to so many rows per group of lanes one workgroup takes them all, and there is no second launch:
-// 128 x 64 fp32 9.8 instead of 11.7 us from call to call, 32 x 1024 bf16 9.9 and 12.0.
+// Up to so many rows per group of lanes and elements in all one workgroup takes them, if there are
+// column sums, and has no second launch: from call to call 128 x 64 fp32 8.7 instead of 11.9 us,
+// 32 x 1024 bf16 9.6 and 12.2, 4 x 8192 fp32 9.1 and 12.0, 3 x 9000 bf16 10.3 and 11.9.  Of rows of 32
+// elements per lane each takes 2 to 4 us: 2 x 16384 bf16 / fp32 10.4 / 12.2 and 12.1 / 11.8, 4 x 9000
+// bf16 12.6 and 11.9, 4 x 16384 bf16 / fp32 17.6 / 21.2 and 12.0 / 12.1 (without column sums 16.5 / 19.7
+// and 7.3).
 constexpr int kAloneRows = 4;
+constexpr int64_t kAloneElems = 32768;
 
 // What goes past the caches.  Results do from 32 MB on, where none of them would stay in the L2s (below,
 // whoever reads them next would lose), if their rows start at even places: 65536 x 512 fp16 forward
@@ -856,12 +864,13 @@ int32_t ss_layernorm_rows_backward(int32_t dtype, int32_t param_dtype, int32_t r
     int n_part = 0;
     if (rows > 0) {
         const int most = most_parts(rows, dim);
+        const bool few = params && (int64_t)rows * dim <= kAloneElems;
 #define SS_ROWS_BWD                                                                           \
     const int threads = kBwdThreads;                                                          \
     const int64_t groups = threads / LANES, need = (rows + groups - 1) / groups;              \
     n_part = (int)(need < most ? need : most);                                                \
     const int wgs = P > 1 ? kBackwardWgs : 2 * kBackwardWgs;                                  \
-    n_part = need <= kAloneRows ? 1 : n_part < wgs ? n_part : wgs;                            \
+    n_part = few && need <= kAloneRows ? 1 : n_part < wgs ? n_part : wgs;                     \
     ProfScope prof("rows_backward_kernel", st);                                               \
     launch(rows_backward_kernel<DT, WT, LANES, P>, dim3(n_part), dim3(threads), st, dy,       \
            dy_stride, x, x_stride, rows, n_valid, gamma, mean, rstd, dx, dx_stride, dim,      \
