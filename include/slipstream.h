@@ -486,6 +486,7 @@ int32_t ss_tensor_list_plan(const ss_tensor *tensors, int32_t n, ss_tensor_list 
  *   grad_scale  what the gradients are to be multiplied by before anything else (the inverse of a
  *               loss scale; 1)
  *   clip        device float[4], 16-byte aligned: norm, factor, 1 if norm is finite else 0, 0
+ *               (finite in fp64: a norm above fp32's range reads inf here, and is still clipped)
  *   ws          device workspace of ss_grad_norm_workspace_bytes(list) bytes, 256-byte aligned
  * The sum has a fixed order: equal inputs give equal bits.  Two calls whose work may overlap need
  * a workspace each.
@@ -501,9 +502,11 @@ int32_t ss_grad_norm(const ss_tensor_list *list, const void *const *grads, doubl
  *     m = beta1 * m + (1 - beta1) * g
  *     v = beta2 * v + (1 - beta2) * g^2
  *     p = p * (1 - lr * weight_decay) - lr / (1 - beta1^t) * m / (sqrt(v / (1 - beta2^t)) + eps)
- * in fp32.  Where clip[2] is 0 (a norm that is not finite) nothing changes but the count of steps
- * left out.  A 16-bit parameter with a master copy is the copy rounded to nearest; without one its
- * own value is read, and the result rounded to nearest.
+ * in fp32; with moments of 8 bits and eps >= 1e-12 by the hardware's root and reciprocal, each
+ * within a step of fp32 of its value (v below 2^-126 counts as 0 in the root).  Where clip[2] is 0
+ * (a norm that is not finite) nothing changes but the count of steps left out.  A 16-bit parameter
+ * with a master copy is the copy rounded to nearest; without one its own value is read, and the
+ * result rounded to nearest.
  *
  * ss_adamw_state (the struct is host memory, what it points to device memory of the caller's):
  *   bits      32: m and v are float [state_elems]
@@ -512,7 +515,8 @@ int32_t ss_grad_norm(const ss_tensor_list *list, const void *const *grads, doubl
  *   master    float [state_elems] or NULL; used for the tensors of 16 bits (the places of the others
  *             are neither read nor written)
  *   counters  SS_ADAMW_COUNTER_BYTES, 64-byte aligned, zeroed before the first step: int64 steps
- *             taken, int64 steps left out, and what belongs to the step in progress.  A step
+ *             taken, int64 steps left out, and what belongs to the step in progress (a count is read
+ *             and set behind the steps before it, on whatever streams they run).  A step
  *             counts itself on the device, so that it can be captured in a graph and replayed;
  *             two steps of one state must not overlap.
  * m, v, exps and master are 16-byte aligned.  All zeros is the state before the first step, in

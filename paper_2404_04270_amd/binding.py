@@ -843,10 +843,11 @@ class TensorList:
     """The tensors of a model (contiguous, fp32 / bf16 / fp16, views at any place of a buffer among
     them), with the work table and the pointer arrays that ss_grad_norm and ss_adamw_step read.
 
-    grads: the gradients, each of its parameter's shape and of its type or fp32; grad_dtypes alone
-    leaves them to set_grads.  With neither, the tensors are taken for gradients themselves (a
+    grads: the gradients, each with its parameter's elements in their order (contiguous) and of its
+    type or fp32; grad_dtypes alone leaves them to set_grads.  With neither, the tensors are taken for gradients themselves (a
     list for ss_grad_norm only).  no_decay: truth values, one per tensor.
-    The work table and a first pointer array are copied here, with the host waiting."""
+    The work table and a first pointer array are copied here, with the host waiting: made once per
+    model (45 us for 16 tensors, 130 for 100, 380 for 400)."""
 
     def __init__(self, params: Sequence[torch.Tensor],
                  grads: Optional[Sequence[torch.Tensor]] = None,
@@ -926,7 +927,9 @@ class TensorList:
 
     def set_grads(self, grads: Sequence[torch.Tensor], stream=None) -> None:
         """The gradients that the calls after this one read, in order on the stream.  Under capture
-        the addresses become part of the graph."""
+        the addresses become part of the graph.  Checking and sending them takes the host 10 us for
+        16 tensors, 31 for 100, 116 for 400: gradients that keep their places (zeroed, not dropped)
+        need it once."""
         _here(self.device, "set_grads")
         ss_pointer_table(self._gptr, self._check_grads(grads), stream)
         self.grads = list(grads)

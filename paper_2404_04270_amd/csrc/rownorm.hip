@@ -5,8 +5,8 @@
 // dx.  A group of lanes owns a row and keeps it in registers, so that every element is read once; the
 // statistics come from the registers in two passes (the mean, then the centred squares: a row whose
 // mean is large against its spread keeps its digits).  Groups are as narrow as the row allows, from
-// one lane to a workgroup of 512; wider rows are read again for each pass, from the caches.  While a
-// group works on a row its next one is being loaded.  The backward pass gives a workgroup rows that
+// one lane to a workgroup of 512; wider rows are read again for each pass, from the caches as long as
+// the rows under way fit them (below).  While a group works on a row its next one is being loaded.  The backward pass gives a workgroup rows that
 // are a grid apart and sums their products column by column in registers; one partial row per
 // workgroup goes to memory, and a second kernel adds those in order.
 //
@@ -14,7 +14,11 @@
 // 16384 x 8192 bf16 89 (6.1), 65536 x 512 fp16 22.7 (5.9), 10007 x 1001 fp32 13.3 (6.0, partly from the
 // last-level cache); backward 32768 x 4096 bf16 139 (5.8), 16384 x 4096 fp32 139 (5.8),
 // 16384 x 1024 bf16 22.2 (4.5), 10007 x 1001 fp16 18 (3.4), each with about 4 us for the second
-// kernel.
+// kernel.  Widths just above a border leave lanes without elements: 16384 x 1025 bf16 21.6 forward and
+// 33.7 backward (1024: 13.0 and 22.5), x 4097 67.7 and 109 (4096: 48.4 and 75.3), 7000 x 9001 fp16 73
+// and 105 (3.4 and 3.6).  Wide rows: 4096 x 20000 bf16 90 and 200 (3.6 and 2.5), 256 x 262144 110 and
+// 221, 64 x 1048576 294 and 581 (0.9 and 0.7: 64 workgroups, and more rows under way than the caches
+// hold).
 #include "elem_io.h"
 #include "ss_common.h"
 
