@@ -157,7 +157,10 @@ def _check(rc: int):
 def _beyond(*sizes: int) -> bool:
     """Whether a size does not fit an int32 argument: ctypes would pass its lower 32 bits on without a
     word, and a smaller problem would be worked on."""
-    return any((n + (1 << 31)) >> 32 for n in sizes)
+    for n in sizes:
+        if not -0x80000000 <= n <= 0x7FFFFFFF:
+            return True
+    return False
 
 
 def _fits(who: str, *sizes: int) -> None:
@@ -345,7 +348,7 @@ def _idx_shape(tables: Tables, idx: torch.Tensor):
     if idx.dim() != 3 or idx.shape[0] != tables.num_tables:
         raise SlipstreamError("idx: need int32 [T, B, L]")
     B, L = int(idx.shape[1]), int(idx.shape[2])
-    if (B | L) >> 31:                    # (in line: a tenth of the time of a call)
+    if (B | L) >> 31:                    # (cheaper than the call)
         _fits("idx", B, L)
     return B, L
 
@@ -844,8 +847,8 @@ class TensorList:
     them), with the work table and the pointer arrays that ss_grad_norm and ss_adamw_step read.
 
     grads: the gradients, each with its parameter's elements in their order (contiguous) and of its
-    type or fp32; grad_dtypes alone leaves them to set_grads.  With neither, the tensors are taken for gradients themselves (a
-    list for ss_grad_norm only).  no_decay: truth values, one per tensor.
+    type or fp32; grad_dtypes alone leaves them to set_grads.  With neither, the tensors are taken
+    for gradients themselves (a list for ss_grad_norm only).  no_decay: truth values, one per tensor.
     The work table and a first pointer array are copied here, with the host waiting: made once per
     model (45 us for 16 tensors, 130 for 100, 380 for 400)."""
 

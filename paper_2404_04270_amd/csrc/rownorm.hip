@@ -6,9 +6,10 @@
 // statistics come from the registers in two passes (the mean, then the centred squares: a row whose
 // mean is large against its spread keeps its digits).  Groups are as narrow as the row allows, from
 // one lane to a workgroup of 512; wider rows are read again for each pass, from the caches as long as
-// the rows under way fit them (below).  While a group works on a row its next one is being loaded.  The backward pass gives a workgroup rows that
-// are a grid apart and sums their products column by column in registers; one partial row per
-// workgroup goes to memory, and a second kernel adds those in order.
+// the rows under way fit them (below).  While a group works on a row its next one is being loaded.
+// The backward pass gives a workgroup rows that are a grid apart and sums their products column by
+// column in registers; one partial row per workgroup goes to memory, and a second kernel adds those
+// in order.
 //
 // us, and TB/s of x, y, dy and dx (a device-wide addition of a constant reaches 6.2): forward
 // 16384 x 8192 bf16 89 (6.1), 65536 x 512 fp16 22.7 (5.9), 10007 x 1001 fp32 13.3 (6.0, partly from the
